@@ -253,6 +253,90 @@ SJD_API int sjd_op_panel_linear_h16_noalloc(int dtype, const void *a_dev, const 
 SJD_API int sjd_op_attention_h16(int dtype, const void *qkv_dev, void *o_dev, int n_samples, int T, int H,
                                  void *hip_stream);
 
+/* ---- Operators beside the flow: queries and keys normed and rotated, a cache in 4 bits, attention over it ----
+ *
+ * For serving conditioners that norm their queries and keys for each head, turn them by positions (of images and clips: row,
+ * column, time) and hold their key/value cache in 4 bits.  They only enqueue work on `hip_stream`: no call here waits, allocates, or keeps
+ * anything, so each can be captured into a graph.  All pointers are DEVICE memory of the current device, rows of `dtype`
+ * (SJD_DTYPE_*) whose heads follow one another, rows `*_stride` ELEMENTS apart; nothing has to start on more than a
+ * multiple of its own element.  No rows (n_rows = 0) is a call that does nothing. */
+
+/* Norms and rotation, in this order.  A norm runs over the head_dim channels of one head of one row:
+ *   norm 0: none;   1: x / sqrt(mean x^2 + eps) * gain (+ shift);   2: (x - mean x) / sqrt(var x + eps) * gain + shift
+ * with gains and shifts [head_dim] float32 (NULL: 1 and 0; they need a norm).  The first rot_dim channels then turn in pairs:
+ * pairing 0 takes channels (i, i + rot_dim / 2), pairing 1 takes (2 i, 2 i + 1), i < rot_dim / 2, and pair i turns by
+ * position * freq_dev[i] radians, (a, b) -> (a cos - b sin, a sin + b cos).  The pairs are dealt to the axes in order, axis_pairs[a] of
+ * them to axis a; each axis has a position of its own (any int32).  Everything in between is computed in float64 and rounded once. */
+typedef struct {
+    int32_t norm;                 /* 0, 1, 2 */
+    float eps;                    /* >= 0 */
+    const float *q_gain_dev, *q_shift_dev, *k_gain_dev, *k_shift_dev;
+    int32_t rot_dim;              /* a multiple of 8, 0 (no rotation) .. head_dim */
+    int32_t pairing;
+    int32_t n_axes;               /* 1..4 where rot_dim > 0 */
+    int32_t axis_pairs[4];        /* >= 0, together rot_dim / 2 */
+    const float *freq_dev;        /* [rot_dim / 2] */
+} sjd_qk_opts;
+
+/* q_out_dev = rotate(norm(q_dev)), and the same for keys; q_dev or k_dev may be NULL (that side is left out).  head_dim a multiple
+ * of 8 up to 256.  pos_dev [n_rows, n_axes] int32.  An output may be its input (same pointer, same stride), else they must not overlap. */
+SJD_API int sjd_op_qk_norm_rope(int dtype, const sjd_qk_opts *opts, const int32_t *pos_dev, const void *q_dev, int64_t q_stride,
+                                int n_heads, const void *k_dev, int64_t k_stride, int n_kv_heads, int head_dim, void *q_out_dev,
+                                int64_t q_out_stride, void *k_out_dev, int64_t k_out_stride, int n_rows, void *hip_stream);
+
+/* A key/value cache of one layer in 4 bits: pages of 64 tokens, pages_dev [n_pages][n_kv_heads][68 * head_dim] bytes on a 16-byte boundary.
+ * 32 consecutive channels of a token and head share a power of two s, the smallest with max |x| <= 7 s, and each is held as 0, 1/2, 1, 3/2,
+ * 2, 3, 4 or 6 times s, with its sign (nearest, ties to the even code; over 6 s: 6 s).  s lies in 2^-23 .. 2^13 for IEEE half rows,
+ * else in 2^-125 .. 2^125; what is held has the type's values exactly.  A group with a NaN or an infinity reads as NaN.
+ * Rows are read in the type they were written in.  The order inside a page is the library's.
+ * head_dim 32, 64, 128 or 256. */
+typedef struct {
+    void *pages_dev;
+    int32_t n_pages, n_kv_heads, head_dim;
+    int32_t dtype;                /* of the rows written and read */
+} sjd_kv4;
+#define SJD_KV4_PAGE 64
+
+/* Keys and values of n_rows tokens into the cache: row i becomes token slot_dev[i] % 64 of page slot_dev[i] / 64 (int32; a slot outside the
+ * cache, such as -1, is left out; a slot given twice holds a mixture of its rows).  opts NULL: as they are.  Otherwise the keys are normed and
+ * rotated first (rounded to dtype, as sjd_op_qk_norm_rope gives them: the cache gets the same bits), and with q_dev (nullable)
+ * the queries of the same rows go to q_out_dev in the same launch; n_kv_heads * head_dim <= 8192 then. */
+SJD_API int sjd_op_kv4_write(const sjd_kv4 *cache, const int32_t *slot_dev, const void *k_dev, int64_t k_stride, const void *v_dev,
+                             int64_t v_stride, int n_rows, const sjd_qk_opts *opts, const int32_t *pos_dev, const void *q_dev,
+                             int64_t q_stride, int n_heads, void *q_out_dev, int64_t q_out_stride, void *hip_stream);
+
+/* Tokens of the cache back in dtype (exactly what is held); zeros for a slot outside the cache. */
+SJD_API int sjd_op_kv4_read(const sjd_kv4 *cache, const int32_t *slot_dev, void *k_dev, int64_t k_stride, void *v_dev,
+                            int64_t v_stride, int n_rows, void *hip_stream);
+
+/* Attention of new tokens over the cache.  Sequence b has kv_len_dev[b] keys, key t being token t % 64 of page
+ * page_table_dev[b * table_stride + t / 64], and the rows q_start_dev[b] .. q_start_dev[b+1] - 1 of q_dev as its last tokens (their own keys are in
+ * the cache); q_start_dev NULL: max_q rows each.  Row i of n sees keys 0 .. kv_len - n + i (causal) or all kv_len of them,
+ * of those without the skip_nearest last ones (the masked probe's o), of those the last `window` (0: all).  Query head h reads key head
+ * h / (n_heads / n_kv_heads).  Scores are scaled by `scale`.  A row that sees no key, or none with a score above -inf, gets zeros.  Keys
+ * on pages that the cache does not have are not seen.  A sequence's rows beyond max_q are left as they are, its keys beyond max_kv and
+ * max_pages pages do not count; rows of no sequence are left as they are.
+ * Long sequences are cut in pieces that are joined in order in a second launch; how they are cut depends on the struct's numbers alone, and
+ * the same call gives the same bits.  The pieces need a workspace (see below) that is the call's own until its work has ended. */
+typedef struct {
+    const void *q_dev;            /* [n_rows][n_heads * head_dim] */
+    void *o_dev;
+    int64_t q_stride, o_stride, table_stride;
+    const int32_t *q_start_dev;   /* [n_seqs + 1], nullable */
+    const int32_t *kv_len_dev;    /* [n_seqs] */
+    const int32_t *page_table_dev;
+    int32_t n_seqs, n_heads, n_rows;
+    int32_t max_pages;            /* entries of a sequence's row of the table */
+    int32_t max_q, max_kv;        /* bounds of what q_start_dev and kv_len_dev hold */
+    int32_t causal, skip_nearest, window;
+    float scale;                  /* > 0 */
+    void *workspace_dev;          /* 16-byte boundary; may be NULL where none is needed */
+    size_t workspace_bytes;
+} sjd_kv4_attention;
+/* Bytes of workspace that sjd_op_kv4_attention needs for these numbers (the struct's pointers are not looked at). */
+SJD_API int sjd_kv4_attention_workspace(const sjd_kv4 *cache, const sjd_kv4_attention *args, size_t *bytes);
+SJD_API int sjd_op_kv4_attention(const sjd_kv4 *cache, const sjd_kv4_attention *args, void *hip_stream);
+
 /* Which kernels the whole-sequence passes of a 16-bit flow use for their projections: 0 automatic (by shape: tile
  * and persistent kernels; the MLP input of large passes on the one with two workgroups per CU; for width 512 between
  * 10240 and 16384 rows the activation-stationary kernels for all but the MLP input), 1 tile and persistent kernels

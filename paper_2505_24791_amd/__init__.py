@@ -30,7 +30,8 @@ PROF_DECODE_GEMM_ALL = (PROF_DECODE_GEMM, PROF_DECODE_RESID, PROF_DECODE_FC1, PR
 EXPORTS = ("sjd_flow_create", "sjd_flow_load_weights", "sjd_jacobi_inverse_block", "sjd_sequential_inverse_block",
            "sjd_sample", "sjd_conditioner", "sjd_op_linear_h16", "sjd_jacobi_trace_block", "sjd_forward_block",
            "sjd_forward", "sjd_flow_set_mask_nearest", "sjd_flow_set_sequential_path", "sjd_flow_set_sequential_cus", "sjd_flow_set_projection_path",
-           "sjd_op_panel_linear_h16", "sjd_op_panel_linear_h16_noalloc", "sjd_op_attention_h16", "sjd_profile_enable", "sjd_profile_read", "sjd_flow_device_bytes",
+           "sjd_op_panel_linear_h16", "sjd_op_panel_linear_h16_noalloc", "sjd_op_attention_h16", "sjd_op_qk_norm_rope", "sjd_op_kv4_write",
+           "sjd_op_kv4_read", "sjd_op_kv4_attention", "sjd_kv4_attention_workspace", "sjd_profile_enable", "sjd_profile_read", "sjd_flow_device_bytes",
            "sjd_last_error", "sjd_flow_destroy")
 
 
@@ -52,6 +53,24 @@ class SjdStats(C.Structure):
 class SjdProfile(C.Structure):
     _fields_ = [("ms", C.c_double * PROF_FAMILIES), ("launches", C.c_int64 * PROF_FAMILIES),
                 ("flops", C.c_double * PROF_FAMILIES), ("bytes", C.c_double * PROF_FAMILIES)]
+
+
+class SjdQkOpts(C.Structure):
+    _fields_ = [("norm", C.c_int32), ("eps", C.c_float), ("q_gain", C.c_void_p), ("q_shift", C.c_void_p), ("k_gain", C.c_void_p),
+                ("k_shift", C.c_void_p), ("rot_dim", C.c_int32), ("pairing", C.c_int32), ("n_axes", C.c_int32),
+                ("axis_pairs", C.c_int32 * 4), ("freq", C.c_void_p)]
+
+
+class SjdKv4(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class SjdKv4Attention(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("o", C.c_void_p), ("q_stride", C.c_int64), ("o_stride", C.c_int64), ("table_stride", C.c_int64),
+                ("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("page_table", C.c_void_p),
+                ("n_seqs", C.c_int32), ("n_heads", C.c_int32), ("n_rows", C.c_int32), ("max_pages", C.c_int32), ("max_q", C.c_int32),
+                ("max_kv", C.c_int32), ("causal", C.c_int32), ("skip_nearest", C.c_int32), ("window", C.c_int32), ("scale", C.c_float),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
 class SjdError(RuntimeError):
@@ -89,6 +108,12 @@ def load_library() -> C.CDLL:
     lib.sjd_flow_set_mask_nearest.argtypes = [vp, C.c_int]
     lib.sjd_op_linear_h16.argtypes = [C.c_int, C.c_int, vp, vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, vp]
     lib.sjd_op_attention_h16.argtypes = [C.c_int, vp, vp, C.c_int, C.c_int, C.c_int, vp]
+    lib.sjd_op_qk_norm_rope.argtypes = [C.c_int, vp, vp, vp, C.c_int64, C.c_int, vp, C.c_int64, C.c_int, C.c_int, vp, C.c_int64, vp,
+                                        C.c_int64, C.c_int, vp]
+    lib.sjd_op_kv4_write.argtypes = [vp, vp, vp, C.c_int64, vp, C.c_int64, C.c_int, vp, vp, vp, C.c_int64, C.c_int, vp, C.c_int64, vp]
+    lib.sjd_op_kv4_read.argtypes = [vp, vp, vp, C.c_int64, vp, C.c_int64, C.c_int, vp]
+    lib.sjd_op_kv4_attention.argtypes = [vp, vp, vp]
+    lib.sjd_kv4_attention_workspace.argtypes = [vp, vp, C.POINTER(C.c_size_t)]
     lib.sjd_profile_enable.argtypes = [vp, C.c_uint32]
     lib.sjd_profile_read.argtypes = [vp, C.POINTER(SjdProfile), C.c_int]
     lib.sjd_flow_device_bytes.argtypes = [vp]
@@ -187,6 +212,195 @@ def op_attention_h16(qkv, n_samples, T, H):
     _check(lib.sjd_op_attention_h16(dtype, C.c_void_p(qkv.data_ptr()), C.c_void_p(o.data_ptr()), n_samples, T, H,
                                     _stream_ptr()))
     return o
+
+
+KV4_PAGE = 64          # tokens of a page of the 4-bit cache
+_NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
+
+
+def _row_dtype(torch_dtype) -> int:
+    import torch
+    got = {torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}.get(torch_dtype)
+    _need(got is not None, f"rows must be float16, bfloat16 or float32, not {torch_dtype}")
+    return got
+
+
+def _need(ok, what: str) -> None:
+    if not ok:
+        raise SjdError(SJD_EINVAL, what)
+
+
+def _rows3(t, what: str, dtype, device):
+    """A tensor [rows, heads, head_dim] whose heads follow one another (any row stride)."""
+    _need(t.is_cuda and t.device == device and t.dtype == dtype, f"{what}: need a {dtype} tensor on {device}")
+    _need(t.dim() == 3, f"{what}: need [rows, heads, head_dim]")
+    n, h, d = t.shape
+    _need(n == 0 or ((d == 1 or t.stride(2) == 1) and (h == 1 or t.stride(1) == d)), f"{what}: the heads of a row must follow one another")
+    return t
+
+
+def _ints(t, what: str, shape, device):
+    import torch
+    _need(t.is_cuda and t.device == device and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == tuple(shape),
+          f"{what}: need a contiguous int32 tensor {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _launch(device, fn, *args) -> None:
+    """Calls fn(*args, stream) with the tensors' device current, on that device's current stream."""
+    import torch
+    if device.index == torch.cuda.current_device():
+        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+
+
+class QkOpts:
+    """Norms and rotation of queries and keys (``sjd_qk_opts``), made once and used by many calls; it holds on to its tensors.
+
+    ``norm``: "none", "rms" or "layer" over the channels of a head, with gains and shifts [head_dim] float32 or None.  ``axis_pairs``: how
+    many channel pairs each axis of the positions turns, together ``rot_dim / 2``; ``freq`` [rot_dim / 2] float32: radians per step of
+    position.  ``adjacent``: pairs are (2i, 2i+1) instead of (i, i + rot_dim / 2)."""
+
+    def __init__(self, *, norm: Optional[str] = "rms", eps: float = 1e-6, q_gain=None, q_shift=None, k_gain=None, k_shift=None,
+                 rot_dim: int = 0, adjacent: bool = False, axis_pairs: Tuple[int, ...] = (), freq=None):
+        import torch
+        _need(norm in _NORMS, f"norm must be one of {[n for n in _NORMS if n]}")
+        _need(rot_dim == 0 or (1 <= len(axis_pairs) <= 4 and freq is not None), "a rotation needs axis_pairs of 1 to 4 axes and freq")
+        self.tensors = {"q_gain": q_gain, "q_shift": q_shift, "k_gain": k_gain, "k_shift": k_shift, "freq": freq}
+        for name, t in self.tensors.items():
+            _need(t is None or (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 1),
+                  f"{name}: need a contiguous float32 vector on the GPU")
+        _need(freq is None or freq.numel() == rot_dim // 2, "freq: need rot_dim / 2 values")
+        self.n_axes = len(axis_pairs) if rot_dim else 0
+        ptr = lambda t: t.data_ptr() if t is not None else None
+        self.c = SjdQkOpts(_NORMS[norm], eps, ptr(q_gain), ptr(q_shift), ptr(k_gain), ptr(k_shift), rot_dim, 1 if adjacent else 0,
+                           self.n_axes, (C.c_int32 * 4)(*axis_pairs[:4]), ptr(freq))
+
+    def checked(self, head_dim: int, device):
+        """The struct's address, for rows of this head size on this device."""
+        for name, t in self.tensors.items():
+            _need(t is None or (t.device == device and (name == "freq" or t.numel() == head_dim)), f"{name}: need {head_dim} values on {device}")
+        return C.addressof(self.c)
+
+
+def op_qk_norm_rope(q, k, pos, opts: QkOpts, *, q_out=None, k_out=None):
+    """``sjd_op_qk_norm_rope``: q [rows, heads, head_dim] and k [rows, kv_heads, head_dim] (either may be None; views of a fused projection's
+    rows as they are), pos [rows, axes] int32 (None without a rotation).  Returns (q_out, k_out), new tensors unless given; an output
+    may be its input."""
+    import torch
+    some = q if q is not None else k
+    _need(some is not None, "need q or k")
+    dtype, device = some.dtype, some.device
+    code = _row_dtype(dtype)
+    args = []
+    n, _, dim = _rows3(some, "q" if q is not None else "k", dtype, device).shape
+    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            args.append((None, 0, 0, None, 0, None))
+            continue
+        _need(_rows3(x, what, dtype, device).shape[0] == n and x.shape[2] == dim, f"{what}: other rows or another head size than q")
+        if out is None:
+            out = torch.empty(x.shape, dtype=dtype, device=device)
+        _need(_rows3(out, what + "_out", dtype, device).shape == x.shape, f"{what}_out: need the shape of {what}")
+        args.append((x.data_ptr(), x.stride(0), x.shape[1], out.data_ptr(), out.stride(0), out))
+    (qp, qs, qh, qo, qos, q_out), (kp, ks, kh, ko, kos, k_out) = args
+    p = _ints(pos, "pos", (n, opts.n_axes), device) if opts.n_axes else None
+    _launch(device, load_library().sjd_op_qk_norm_rope, code, opts.checked(dim, device), p, qp, qs, qh, kp, ks, kh, dim, qo, qos, ko, kos, n)
+    return q_out, k_out
+
+
+class Kv4Cache:
+    """A key/value cache of one layer in 4 bits (``sjd_kv4``): ``pages`` uint8 [pages, kv_heads, 68 * head_dim], 64 tokens to a page, of rows
+    of ``dtype``.  The pages are the caller's: any tensor of that shape, e.g. ``Kv4Cache.zeros(...)``."""
+
+    def __init__(self, pages, dtype):
+        import torch
+        _need(pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous() and pages.dim() == 3 and pages.shape[2] % 68 == 0,
+              "pages: need a contiguous uint8 tensor [pages, kv_heads, 68 * head_dim] on the GPU")
+        self.pages, self.dtype, self.device = pages, dtype, pages.device
+        self.n_pages, self.kv_heads, self.head_dim = pages.shape[0], pages.shape[1], pages.shape[2] // 68
+        self.c = SjdKv4(pages.data_ptr(), self.n_pages, self.kv_heads, self.head_dim, _row_dtype(dtype))
+        self.address = C.addressof(self.c)
+
+    @classmethod
+    def zeros(cls, n_pages: int, kv_heads: int, head_dim: int, dtype, device="cuda"):
+        import torch
+        return cls(torch.zeros((n_pages, kv_heads, 68 * head_dim), dtype=torch.uint8, device=device), dtype)
+
+    def _kv(self, t, what: str, n: int):
+        _need(tuple(_rows3(t, what, self.dtype, self.device).shape) == (n, self.kv_heads, self.head_dim),
+              f"{what}: need [{n}, {self.kv_heads}, {self.head_dim}]")
+        return t.data_ptr(), t.stride(0)
+
+
+def op_kv4_write(cache: Kv4Cache, k, v, slot, *, opts: Optional[QkOpts] = None, pos=None, q=None, q_out=None):
+    """``sjd_op_kv4_write``: rows k, v [rows, kv_heads, head_dim] become the tokens ``slot`` [rows] int32 (page * 64 + offset; -1: left out).
+    With ``opts`` the keys are normed and rotated first, and with ``q`` [rows, heads, head_dim] the queries of those rows too: returns them
+    (``q_out`` or a new tensor), else None."""
+    import torch
+    n = k.shape[0]
+    (kp, ks), (vp_, vs) = cache._kv(k, "k", n), cache._kv(v, "v", n)
+    sp = _ints(slot, "slot", (n,), cache.device)
+    op = pp = qp = qo = None
+    qs = qos = heads = 0
+    if opts is not None:
+        op = opts.checked(cache.head_dim, cache.device)
+        pp = _ints(pos, "pos", (n, opts.n_axes), cache.device) if opts.n_axes else None
+    if q is not None:
+        _need(opts is not None, "queries need opts")
+        _need(_rows3(q, "q", cache.dtype, cache.device).shape[0] == n and q.shape[2] == cache.head_dim, "q: other rows or another head size")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        _need(_rows3(q_out, "q_out", cache.dtype, cache.device).shape == q.shape, "q_out: need the shape of q")
+        qp, qs, heads, qo, qos = q.data_ptr(), q.stride(0), q.shape[1], q_out.data_ptr(), q_out.stride(0)
+    _launch(cache.device, load_library().sjd_op_kv4_write, cache.address, sp, kp, ks, vp_, vs, n, op, pp, qp, qs, heads, qo, qos)
+    return q_out if q is not None else None
+
+
+def op_kv4_read(cache: Kv4Cache, slot, *, k_out=None, v_out=None):
+    """``sjd_op_kv4_read``: the tokens ``slot`` [rows] int32 of the cache, (k, v) [rows, kv_heads, head_dim]; zeros for a slot outside it."""
+    import torch
+    n = slot.shape[0]
+    sp = _ints(slot, "slot", (n,), cache.device)
+    k_out, v_out = (torch.empty((n, cache.kv_heads, cache.head_dim), dtype=cache.dtype, device=cache.device) if t is None else t
+                    for t in (k_out, v_out))
+    (kp, ks), (vp_, vs) = cache._kv(k_out, "k_out", n), cache._kv(v_out, "v_out", n)
+    _launch(cache.device, load_library().sjd_op_kv4_read, cache.address, sp, kp, ks, vp_, vs, n)
+    return k_out, v_out
+
+
+def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, max_q: int = 1, max_kv: Optional[int] = None,
+                     causal: bool = True, skip_nearest: int = 0, window: int = 0, scale: Optional[float] = None, out=None):
+    """``sjd_op_kv4_attention``: q [rows, heads, head_dim], the last tokens of sequences with ``kv_len`` [seqs] int32 cached keys on the pages
+    page_table [seqs, max_pages] int32; sequence b has the rows q_start[b] .. q_start[b+1] - 1 (q_start [seqs + 1] int32; None: max_q
+    each).  max_q and max_kv bound the rows and keys of a sequence (max_kv None: all that the table has room for).  Rows of no
+    sequence are left as they are in ``out`` (None: a new tensor, which holds anything there)."""
+    import math
+    import torch
+    n, heads, dim = _rows3(q, "q", cache.dtype, cache.device).shape
+    _need(dim == cache.head_dim, "q: another head size than the cache's")
+    _need(page_table.dim() == 2 and kv_len.dim() == 1 and page_table.shape[0] == kv_len.shape[0], "need page_table [seqs, max_pages] and kv_len [seqs]")
+    seqs, pages = page_table.shape
+    _need(page_table.is_cuda and page_table.device == cache.device and page_table.dtype == torch.int32 and (pages <= 1 or page_table.stride(1) == 1),
+          "page_table: need int32 rows on the cache's device")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _need(_rows3(out, "out", cache.dtype, cache.device).shape == q.shape, "out: need the shape of q")
+    a = SjdKv4Attention(q.data_ptr(), out.data_ptr(), q.stride(0), out.stride(0), page_table.stride(0),
+                        _ints(q_start, "q_start", (seqs + 1,), cache.device) if q_start is not None else None,
+                        _ints(kv_len, "kv_len", (seqs,), cache.device), page_table.data_ptr(), seqs, heads, n, pages, max_q,
+                        pages * KV4_PAGE if max_kv is None else max_kv, 1 if causal else 0, skip_nearest, window,
+                        1.0 / math.sqrt(dim) if scale is None else scale, None, 0)
+    lib = load_library()
+    need = C.c_size_t(0)
+    _check(lib.sjd_kv4_attention_workspace(cache.address, C.addressof(a), C.byref(need)))
+    if need.value:
+        ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
+        a.workspace, a.workspace_bytes = ws.data_ptr(), need.value
+    _launch(cache.device, lib.sjd_op_kv4_attention, cache.address, C.addressof(a))
+    return out
 
 
 class Flow:

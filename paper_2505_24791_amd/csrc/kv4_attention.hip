@@ -1,0 +1,362 @@
+// Attention of new tokens over a key/value cache held in 4 bits.
+//
+//   o_r = sum_t p_rt v_t / sum_t p_rt,   p_rt = exp(scale q_r . k_t - m_r),   over the keys t that row r sees
+//
+// One pass over the cache with the running maximum and sum of the softmax.  A key or value is a 4-bit float times a power of two and
+// converts exactly to 16 bits, so the products on the matrix unit have exact right operands; only the probabilities are rounded, to the
+// type of the rows (float32 rows: every left operand as three bfloat16 pieces, which hold its 24 bits, on the same instruction).
+#include "kv4.h"
+
+namespace sjd {
+
+namespace {
+
+template <typename T> struct Op { typedef T t; static constexpr int pieces = 1; };
+template <> struct Op<float> { typedef bf16 t; static constexpr int pieces = 3; };
+
+typedef uint32_t u32;
+
+// two values (a byte) of w with the scale s
+template <typename HT, int SEL> __device__ __forceinline__ void decode2(u32 w, float s, HT &a, HT &b) {
+    if constexpr (__is_same(HT, f16)) {
+        const auto x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, SEL);
+        a = x[0]; b = x[1];
+    } else {
+        const auto x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, SEL);
+        a = x[0]; b = x[1];
+    }
+}
+template <typename HT> __device__ __forceinline__ void decode8(u32 w, float s, typename Half16<HT>::v8 &x) {
+    HT a, b;
+    decode2<HT, 0>(w, s, a, b); x[0] = a; x[1] = b;
+    decode2<HT, 1>(w, s, a, b); x[2] = a; x[3] = b;
+    decode2<HT, 2>(w, s, a, b); x[4] = a; x[5] = b;
+    decode2<HT, 3>(w, s, a, b); x[6] = a; x[7] = b;
+}
+__device__ __forceinline__ float pow2_byte(u32 w, int i) { return __uint_as_float(((w >> (8 * i)) & 255u) << 23); }
+
+// x as a sum of `n` values of the operand type, the largest first
+template <typename T, int N> __device__ __forceinline__ void split(float x, typename Op<T>::t (&p)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        p[i] = from_f32<typename Op<T>::t>(x);
+        x -= to_f32<typename Op<T>::t>(p[i]);
+    }
+}
+
+// over the four lanes of a row (16 lanes apart)
+__device__ __forceinline__ float row_max(float v) {
+    v = fmaxf(v, __shfl_xor(v, 16, 64));
+    return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+__device__ __forceinline__ float row_sum(float v) {
+    v += __shfl_xor(v, 16, 64);
+    return v + __shfl_xor(v, 32, 64);
+}
+
+struct Seq { int row0, n, len; };      // first row, rows and keys of a sequence, within what the call allows
+__device__ __forceinline__ Seq sequence(const Kv4Attn &a, int b) {
+    Seq s;
+    if (a.q_start) {
+        s.row0 = min(max(a.q_start[b], 0), a.n_rows);
+        s.n = min(min(max(a.q_start[b + 1], s.row0), a.n_rows) - s.row0, a.max_q);
+    } else {
+        s.row0 = b * a.max_q;
+        s.n = a.max_q;
+    }
+    s.len = min(min(max(a.kv_len[b], 0), a.max_kv), a.max_pages * kKv4Page);
+    return s;
+}
+// keys first .. last of the i-th new token of a sequence (none: last < first)
+__device__ __forceinline__ void seen(const Kv4Attn &a, const Seq &s, int i, int &first, int &last) {
+    last = (a.causal ? s.len - s.n + i : s.len - 1) - a.skip;
+    first = a.window ? max(0, last - a.window + 1) : 0;
+    last = max(last, -1);
+}
+
+// ------------------------------------------------------------------------------------------------
+// Up to 16 rows (new tokens times query heads of one key head) a workgroup, the pages of its piece of the sequence dealt to four
+// waves.  S^T = K Q^T, 16 tokens an instruction: a lane holds row lane % 16 and, of a subtile, tokens 4 (lane / 16) + 0..3, which is
+// the right operand of O^T = V^T P^T as it stands, two subtiles to an instruction.
+constexpr int kRows = 16;
+
+struct Tile { int first_lo, last_lo, first_hi, last_hi; };      // what the tile's first and last row see
+__device__ __forceinline__ Tile tile_range(const Kv4Attn &a, const Seq &s, int r0, int n_r, int G) {
+    Tile t;
+    seen(a, s, r0 / G, t.first_lo, t.last_lo);
+    seen(a, s, (min(r0 + kRows, n_r) - 1) / G, t.first_hi, t.last_hi);
+    return t;
+}
+
+template <typename T, int NG>
+__global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Attn a, int n_tiles) {
+    typedef typename Op<T>::t HT;
+    typedef typename Half16<HT>::v8 v8;
+    typedef T qv8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    constexpr int NP = Op<T>::pieces, DIM = 32 * NG;
+    constexpr int RG = NG < 4 ? NG : 4, RDIM = 32 * RG, LD = RDIM + 4;      // groups joined at a time
+    __shared__ __attribute__((aligned(16))) float acc[4][kRows * LD];
+    __shared__ float ms[4][kRows], ls[4][kRows];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
+    const int G = a.n_heads / a.cache.n_heads;
+    const int part = blockIdx.x % a.n_splits, tile = blockIdx.x / a.n_splits % n_tiles, pair = blockIdx.x / a.n_splits / n_tiles;
+    const int b = pair / a.cache.n_heads, h = pair % a.cache.n_heads;
+    const Seq sq = sequence(a, b);
+    const int n_r = sq.n * G, r0 = tile * kRows;
+    if (r0 >= n_r) return;
+    const Tile tr = tile_range(a, sq, r0, n_r, G);
+    const int lo = tr.first_lo, hi = tr.last_hi;
+    const int p0 = max(lo / kKv4Page, part * a.split_pages);
+    const int p1 = min(hi < lo ? 0 : hi / kKv4Page + 1, (part + 1) * a.split_pages);
+    if (p0 >= p1 && a.n_splits > 1) return;
+    const int row = min(r0 + r, n_r - 1);
+    int first, last;
+    seen(a, sq, row / G, first, last);
+
+    v8 qf[NG][NP];
+    {
+        const T *q = (const T *)a.q + (int64_t)(sq.row0 + row / G) * a.q_stride + (int64_t)(h * G + row % G) * DIM;
+#pragma unroll
+        for (int s = 0; s < NG; ++s) {
+            const qv8 x = *reinterpret_cast<const qv8 *>(q + 8 * (j * NG + s));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                HT p[NP];
+                if constexpr (NP == 1) p[0] = x[e];
+                else split<T, NP>(x[e], p);
+#pragma unroll
+                for (int c = 0; c < NP; ++c) qf[s][c][e] = p[c];
+            }
+        }
+    }
+    f32x4v o[NG][2];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) o[g][0] = o[g][1] = f32x4v{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;                 // of the row (m scaled, base 2); of the lane's tokens of the row
+
+    for (int page = p0 + wave; page < p1; page += 4) {
+        const int id = a.table[b * a.table_stride + page];
+        if (id < 0 || id >= a.cache.n_pages) continue;
+        const uint8_t *blk = a.cache.pages + ((size_t)id * a.cache.n_heads + h) * kv4_block_bytes(DIM);
+        const int t0 = page * kKv4Page;
+        const bool full = t0 >= tr.first_hi && t0 + kKv4Page - 1 <= tr.last_lo;      // every row sees the whole page
+
+        f32x4v sc[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            sc[t] = f32x4v{0.f, 0.f, 0.f, 0.f};
+            const u32 *k = reinterpret_cast<const u32 *>(blk + kv4_k_code(DIM, 16 * t + r, j * NG));
+#pragma unroll
+            for (int s = 0; s < NG; ++s) {
+                const u32 ks = *reinterpret_cast<const u32 *>(blk + kv4_k_scale(DIM, r, (j * NG + s) / 4));
+                v8 kf;
+                decode8<HT>(k[s], pow2_byte(ks, t), kf);
+#pragma unroll
+                for (int c = 0; c < NP; ++c) sc[t] = Mfma16<HT>::run(kf, qf[s][c], sc[t]);
+            }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int key = t0 + 16 * t + 4 * j + e;
+                if (!full && !(key >= first && key <= last)) sc[t][e] = -INFINITY;
+                mx = fmaxf(mx, sc[t][e]);
+            }
+        const float m_new = fmaxf(m, row_max(mx) * a.scale_log2);
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        if (__builtin_amdgcn_ballot_w64(m_new != m) != 0) {
+            const float corr = __builtin_amdgcn_exp2f(m - m_use);
+            l *= corr;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[g][c][e] *= corr;
+            m = m_new;
+        }
+        bool nan_hidden = false;
+#pragma unroll
+        for (int t = 0; t < 4; t += 2) {
+            v8 pf[NP];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(sc[t + e / 4][e % 4], a.scale_log2, -m_use));
+                HT p[NP];
+                if constexpr (NP == 1) p[0] = from_f32<HT>(x);
+                else { split<T, NP>(x, p); l += x; }
+#pragma unroll
+                for (int c = 0; c < NP; ++c) pf[c][e] = p[c];
+            }
+            if constexpr (NP == 1) l = Half16<HT>::add_all(pf[0], l);
+            u32 vw[2][NG], vs[2][NG];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const u32 *v = reinterpret_cast<const u32 *>(blk + kv4_v_code(DIM, 16 * (t + u) + 4 * j, r));
+                const u32 *s = reinterpret_cast<const u32 *>(blk + kv4_v_scale(DIM, 16 * (t + u) + 4 * j));
+#pragma unroll
+                for (int g = 0; g < NG; ++g) { vw[u][g] = v[g]; vs[u][g] = s[g]; }
+            }
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                v8 vf[2];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = (e % 4) * NG + g;
+                    float s = pow2_byte(vs[e / 4][at / 4], at % 4);
+                    if (!full) {
+                        // what no row sees is nothing's, and may be anything; a NaN that some row sees must not reach the others as 0 * NaN
+                        const int key = t0 + 16 * (t + e / 4) + 4 * j + e % 4;
+                        if (!(key >= lo && key <= hi)) s = 0.f;
+                        else if (s == INFINITY) { s = 0.f; nan_hidden = true; }
+                    }
+                    HT x0, x1;
+                    const u32 w = vw[e / 4][at / 4];
+                    if (at % 4 == 0) decode2<HT, 0>(w, s, x0, x1);
+                    else if (at % 4 == 1) decode2<HT, 1>(w, s, x0, x1);
+                    else if (at % 4 == 2) decode2<HT, 2>(w, s, x0, x1);
+                    else decode2<HT, 3>(w, s, x0, x1);
+                    vf[0][e] = x0;
+                    vf[1][e] = x1;
+                }
+#pragma unroll
+                for (int c = 0; c < NP; ++c) {
+                    o[g][0] = Mfma16<HT>::run(vf[0], pf[c], o[g][0]);
+                    o[g][1] = Mfma16<HT>::run(vf[1], pf[c], o[g][1]);
+                }
+            }
+        }
+        if (!full && __builtin_amdgcn_ballot_w64(nan_hidden) != 0) {
+            for (int off = 0; off < kKv4Page; ++off)
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+                    if (t0 + off >= first && t0 + off <= last && blk[kv4_v_scale(DIM, off) + g] == 255)
+                        o[g][0] = o[g][1] = f32x4v{NAN, NAN, NAN, NAN};
+        }
+    }
+    l = row_sum(l);
+    if (j == 0) { ms[wave][r] = m; ls[wave][r] = l; }
+
+    // the four waves' sums, RG groups at a time
+    const int orow = threadIdx.x >> 4, oc = threadIdx.x & 15;      // 16 threads a row, RDIM / 16 channels each
+    constexpr int PER = RDIM / 16;
+    const bool live = r0 + orow < n_r;
+    const int64_t at = sq.row0 + (r0 + orow) / G;
+    const int head = h * G + (r0 + orow) % G;
+#pragma unroll
+    for (int g0 = 0; g0 < NG; g0 += RG) {
+        if (g0) __syncthreads();
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            float *d = &acc[wave][r * LD + 32 * g + 8 * j];
+            const f32x4v x = o[g0 + g][0], y = o[g0 + g][1];
+            *reinterpret_cast<f32x4 *>(d) = f32x4{x[0], y[0], x[1], y[1]};
+            *reinterpret_cast<f32x4 *>(d + 4) = f32x4{x[2], y[2], x[3], y[3]};
+        }
+        __syncthreads();
+        const float mj = fmaxf(fmaxf(ms[0][orow], ms[1][orow]), fmaxf(ms[2][orow], ms[3][orow]));
+        const float mu = mj == -INFINITY ? 0.f : mj;
+        float w[4], den = 0.f, sum[PER];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { w[i] = __builtin_amdgcn_exp2f(ms[i][orow] - mu); den = fmaf(w[i], ls[i][orow], den); }
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            sum[e] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[e] = fmaf(w[i], acc[i][orow * LD + oc * PER + e], sum[e]);
+        }
+        if (!live) continue;
+        if (a.n_splits == 1) {
+            T *out = (T *)a.o + at * a.o_stride + (int64_t)head * DIM + 32 * g0 + oc * PER;
+            const float inv = den == 0.f ? 0.f : 1.f / den;
+#pragma unroll
+            for (int e = 0; e < PER; ++e) out[e] = from_f32<T>(den == 0.f ? 0.f : sum[e] * inv);
+        } else {
+            float *out = a.partial + ((at * a.n_heads + head) * a.n_splits + part) * (DIM + 2);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) out[32 * g0 + oc * PER + e] = sum[e];
+            if (g0 == 0 && oc == 0) { out[DIM] = mj; out[DIM + 1] = den; }
+        }
+    }
+}
+
+// Joins the pieces of one row and head: a wave each, in the order of the pieces.
+template <typename T>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
+    const int G = a.n_heads / a.cache.n_heads, dim = a.cache.dim, lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int i = (int)(id % a.max_q);
+    const int head = (int)(id / a.max_q % a.n_heads);
+    const int64_t b = id / a.max_q / a.n_heads;
+    if (b >= a.n_seqs) return;
+    const Seq sq = sequence(a, (int)b);
+    if (i >= sq.n) return;
+    const Tile tr = tile_range(a, sq, (i * G + head % G) / kRows * kRows, sq.n * G, G);
+    const int lo = tr.first_lo, hi = tr.last_hi;
+    const int s0 = lo / kKv4Page / a.split_pages, s1 = hi < lo ? s0 : hi / kKv4Page / a.split_pages + 1;
+    const int64_t at = sq.row0 + i;
+    const float *p = a.partial + (at * a.n_heads + head) * a.n_splits * (dim + 2);
+    float m = -INFINITY;
+    for (int s = s0 + lane; s < s1; s += 64) m = fmaxf(m, p[(int64_t)s * (dim + 2) + dim]);
+    m = wave_max(m);
+    const float mu = m == -INFINITY ? 0.f : m;
+    float den = 0.f, sum[4] = {};
+    for (int s = s0; s < s1; ++s) {
+        const float *ps = p + (int64_t)s * (dim + 2);
+        const float w = __builtin_amdgcn_exp2f(ps[dim] - mu);
+        den = fmaf(w, ps[dim + 1], den);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (lane + 64 * c < dim) sum[c] = fmaf(w, ps[lane + 64 * c], sum[c]);
+    }
+    T *out = (T *)a.o + at * a.o_stride + (int64_t)head * dim;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (lane + 64 * c < dim) out[lane + 64 * c] = from_f32<T>(den == 0.f ? 0.f : sum[c] / den);
+}
+
+int row_tiles(const Kv4Attn &a) { return (int)(((int64_t)a.max_q * (a.n_heads / a.cache.n_heads) + kRows - 1) / kRows); }
+
+}  // namespace
+
+void kv4_attention_split(Kv4Attn &a) {
+    const int pages = (a.max_kv + kKv4Page - 1) / kKv4Page;
+    const int64_t have = (int64_t)a.n_seqs * a.cache.n_heads * row_tiles(a);
+    int64_t want = have ? (2048 + have - 1) / have : 1;
+    want = want < 1 ? 1 : want;
+    int per = (int)((pages + want - 1) / want);
+    per = (per + 3) / 4 * 4;                      // a page for each wave
+    a.split_pages = per < 4 ? 4 : per;
+    a.n_splits = (pages + a.split_pages - 1) / a.split_pages;
+    if (a.n_splits < 1) a.n_splits = 1;
+}
+
+int64_t kv4_attention_grid(const Kv4Attn &a) { return (int64_t)a.n_seqs * a.cache.n_heads * row_tiles(a) * a.n_splits; }
+
+size_t kv4_attention_workspace(const Kv4Attn &a) {
+    return a.n_splits > 1 ? (size_t)a.n_rows * a.n_heads * a.n_splits * (a.cache.dim + 2) * sizeof(float) : 0;
+}
+
+template <typename T> void launch_kv4_attention(const Kv4Attn &a, hipStream_t s) {
+    const int n_tiles = row_tiles(a);
+    const int64_t n = kv4_attention_grid(a);
+    if (n <= 0 || a.n_rows <= 0) return;
+    const dim3 grid((unsigned)n), block(256);
+    switch (a.cache.dim / 32) {
+        case 1: hipLaunchKernelGGL((kv4_attention_kernel<T, 1>), grid, block, 0, s, a, n_tiles); break;
+        case 2: hipLaunchKernelGGL((kv4_attention_kernel<T, 2>), grid, block, 0, s, a, n_tiles); break;
+        case 4: hipLaunchKernelGGL((kv4_attention_kernel<T, 4>), grid, block, 0, s, a, n_tiles); break;
+        default: hipLaunchKernelGGL((kv4_attention_kernel<T, 8>), grid, block, 0, s, a, n_tiles); break;
+    }
+    if (a.n_splits > 1) {
+        const int64_t rows = (int64_t)a.n_seqs * a.n_heads * a.max_q;
+        hipLaunchKernelGGL((kv4_join_kernel<T>), dim3((unsigned)((rows + 3) / 4)), block, 0, s, a);
+    }
+}
+template void launch_kv4_attention<float>(const Kv4Attn &, hipStream_t);
+template void launch_kv4_attention<bf16>(const Kv4Attn &, hipStream_t);
+template void launch_kv4_attention<f16>(const Kv4Attn &, hipStream_t);
+
+}  // namespace sjd

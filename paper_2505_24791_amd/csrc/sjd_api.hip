@@ -17,6 +17,7 @@
 
 #include "common.h"
 #include "gemm_rules.h"
+#include "kv4.h"
 #include "seq_groups.h"
 
 using namespace sjd;
@@ -1489,6 +1490,212 @@ int sjd_op_attention_h16(int dtype, const void *qkv_dev, void *o_dev, int n_samp
     else if (dtype == SJD_DTYPE_BF16) launch_flash_attention_h16<bf16>((const bf16 *)qkv_dev, (bf16 *)o_dev, n_samples, T, H, s);
     else launch_flash_attention_h16<f16>((const f16 *)qkv_dev, (f16 *)o_dev, n_samples, T, H, s);
     HIP_TRY(hipStreamSynchronize(s));
+    HIP_TRY(hipGetLastError());
+    return SJD_OK;
+}
+
+// ---- operators beside the flow ------------------------------------------------------------------
+
+namespace {
+
+bool known_dtype(int d) { return d == SJD_DTYPE_F32 || d == SJD_DTYPE_BF16 || d == SJD_DTYPE_F16; }
+
+// rows of n_heads heads: pointer on an element, rows that do not overlap where they are written
+int check_rows(const char *what, int dtype, const void *p, int64_t stride, int64_t width, int n_rows, bool written) {
+    if (!p) return fail(SJD_EINVAL, "null device pointer (%s)", what);
+    if ((uintptr_t)p % (dtype == SJD_DTYPE_F32 ? 4 : 2)) return fail(SJD_EINVAL, "%s does not start on a multiple of its element", what);
+    if (stride < 0 || (written && n_rows > 1 && stride < width)) return fail(SJD_EINVAL, "the row stride of %s is too small", what);
+    return SJD_OK;
+}
+
+int check_qk_opts(const sjd_qk_opts *o, const int32_t *pos, int dim, QkOpts *out) {
+    if (o->norm < 0 || o->norm > 2) return fail(SJD_EINVAL, "norm must be 0, 1 or 2");
+    if (o->norm && !(o->eps >= 0.f && isfinite(o->eps))) return fail(SJD_EINVAL, "eps must be finite and >= 0");
+    if (!o->norm && (o->q_gain_dev || o->q_shift_dev || o->k_gain_dev || o->k_shift_dev)) return fail(SJD_EINVAL, "gains and shifts need a norm");
+    if (o->rot_dim < 0 || o->rot_dim > dim || o->rot_dim % 8) return fail(SJD_EINVAL, "rot_dim must be a multiple of 8 in 0..head_dim");
+    if (o->pairing != 0 && o->pairing != 1) return fail(SJD_EINVAL, "pairing must be 0 or 1");
+    QkOpts q{};
+    q.norm = o->norm; q.eps = o->eps;
+    q.q_gain = o->q_gain_dev; q.q_shift = o->q_shift_dev; q.k_gain = o->k_gain_dev; q.k_shift = o->k_shift_dev;
+    q.rot = o->rot_dim; q.adjacent = o->pairing; q.freq = o->freq_dev;
+    if (o->rot_dim) {
+        if (o->n_axes < 1 || o->n_axes > 4) return fail(SJD_EINVAL, "n_axes must be 1..4");
+        int64_t sum = 0;
+        for (int a = 0; a < o->n_axes; ++a) {
+            if (o->axis_pairs[a] < 0) return fail(SJD_EINVAL, "axis_pairs must not be negative");
+            sum += o->axis_pairs[a];
+            q.axis_end[a] = (int)(sum < dim ? sum : dim);
+        }
+        if (sum != o->rot_dim / 2) return fail(SJD_EINVAL, "axis_pairs must add up to rot_dim / 2");
+        if (!o->freq_dev || !pos) return fail(SJD_EINVAL, "a rotation needs freq_dev and pos_dev");
+        q.n_axes = o->n_axes;
+    }
+    *out = q;
+    return SJD_OK;
+}
+
+int check_cache(const sjd_kv4 *c, Kv4Cache *out) {
+    if (!c) return fail(SJD_EINVAL, "null cache");
+    if (!known_dtype(c->dtype)) return fail(SJD_EINVAL, "unknown dtype %d", c->dtype);
+    if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256)
+        return fail(SJD_EINVAL, "head_dim must be 32, 64, 128 or 256");
+    if (c->n_pages < 1 || c->n_pages > INT32_MAX / SJD_KV4_PAGE || c->n_kv_heads < 1 || c->n_kv_heads > 65535)
+        return fail(SJD_EINVAL, "n_pages (slots are int32) or n_kv_heads out of range");
+    *out = Kv4Cache{(uint8_t *)c->pages_dev, c->n_pages, c->n_kv_heads, c->head_dim};
+    return SJD_OK;
+}
+
+int check_pages(const sjd_kv4 *c) {
+    if (!c->pages_dev || (uintptr_t)c->pages_dev % 16) return fail(SJD_EINVAL, "pages_dev must be given, on a 16-byte boundary");
+    return SJD_OK;
+}
+
+int check_heads(int n_heads, int n_kv) {
+    if (n_kv < 1 || n_heads < 1 || n_heads > 65535 || n_heads % n_kv) return fail(SJD_EINVAL, "n_heads must be a multiple of n_kv_heads, up to 65535");
+    return SJD_OK;
+}
+
+// grids are counted in 31 bits
+int check_work(int64_t n_rows, int64_t heads, int64_t chunks) {
+    if (n_rows < 0) return fail(SJD_EINVAL, "n_rows must not be negative");
+    if (n_rows * heads > (int64_t)INT32_MAX * 8 || n_rows * heads / 256 * chunks + 2 > INT32_MAX) return fail(SJD_EINVAL, "too many rows for one call");
+    return SJD_OK;
+}
+
+int check_attention(const sjd_kv4 *c, const sjd_kv4_attention *g, Kv4Attn *out) {
+    Kv4Attn a{};
+    int rc = check_cache(c, &a.cache);
+    if (rc) return rc;
+    if (!g) return fail(SJD_EINVAL, "null arguments");
+    if ((rc = check_heads(g->n_heads, c->n_kv_heads))) return rc;
+    if (g->n_seqs < 0 || g->n_rows < 0 || g->max_pages < 0 || g->max_q < 0 || g->max_kv < 0) return fail(SJD_EINVAL, "a count is negative");
+    if (g->skip_nearest < 0 || g->window < 0) return fail(SJD_EINVAL, "skip_nearest and window must not be negative");
+    if (!(g->scale > 0.f && isfinite(g->scale))) return fail(SJD_EINVAL, "scale must be finite and above 0");
+    if (!g->q_start_dev && (int64_t)g->n_seqs * g->max_q != g->n_rows) return fail(SJD_EINVAL, "without q_start_dev there are n_seqs * max_q rows");
+    if ((int64_t)g->max_q * g->n_heads > INT32_MAX / 2 || g->max_kv > INT32_MAX / 2 || g->max_pages > INT32_MAX / SJD_KV4_PAGE ||
+        (int64_t)g->n_seqs * g->max_q > (int64_t)1 << 40)
+        return fail(SJD_EINVAL, "max_q, max_kv or max_pages out of range");
+    a.q = g->q_dev; a.o = g->o_dev; a.q_stride = g->q_stride; a.o_stride = g->o_stride; a.table_stride = g->table_stride;
+    a.q_start = g->q_start_dev; a.kv_len = g->kv_len_dev; a.table = g->page_table_dev;
+    a.n_seqs = g->n_seqs; a.n_heads = g->n_heads; a.n_rows = g->n_rows; a.max_pages = g->max_pages;
+    a.max_q = g->max_q < g->n_rows ? g->max_q : g->n_rows;      // no sequence has more rows than there are
+    a.max_kv = (int)((int64_t)g->max_pages * SJD_KV4_PAGE < g->max_kv ? (int64_t)g->max_pages * SJD_KV4_PAGE : g->max_kv);
+    a.causal = g->causal != 0; a.skip = g->skip_nearest; a.window = g->window;
+    a.scale_log2 = g->scale * 1.44269504088896340736f;
+    kv4_attention_split(a);
+    if (kv4_attention_grid(a) > INT32_MAX) return fail(SJD_EINVAL, "too many rows and sequences for one call");
+    *out = a;
+    return SJD_OK;
+}
+
+}  // namespace
+
+int sjd_op_qk_norm_rope(int dtype, const sjd_qk_opts *opts, const int32_t *pos_dev, const void *q_dev, int64_t q_stride,
+                        int n_heads, const void *k_dev, int64_t k_stride, int n_kv_heads, int head_dim, void *q_out_dev,
+                        int64_t q_out_stride, void *k_out_dev, int64_t k_out_stride, int n_rows, void *hip_stream) {
+    if (!known_dtype(dtype)) return fail(SJD_EINVAL, "unknown dtype %d", dtype);
+    if (!opts) return fail(SJD_EINVAL, "null options");
+    if (head_dim < 8 || head_dim > 256 || head_dim % 8) return fail(SJD_EINVAL, "head_dim must be a multiple of 8 in 8..256");
+    if (n_rows == 0) return SJD_OK;
+    if (!q_dev && !k_dev) return fail(SJD_EINVAL, "null device pointer (queries and keys)");
+    if ((q_dev && (n_heads < 1 || n_heads > 65535)) || (k_dev && (n_kv_heads < 1 || n_kv_heads > 65535)))
+        return fail(SJD_EINVAL, "n_heads and n_kv_heads must lie in 1..65535");
+    const int hq = q_dev ? n_heads : 0, hk = k_dev ? n_kv_heads : 0;
+    QkOpts o;
+    int rc;
+    if ((rc = check_work(n_rows, hq + hk, 1)) || (rc = check_qk_opts(opts, pos_dev, head_dim, &o))) return rc;
+    if (q_dev && ((rc = check_rows("q_dev", dtype, q_dev, q_stride, (int64_t)hq * head_dim, n_rows, false)) ||
+                  (rc = check_rows("q_out_dev", dtype, q_out_dev, q_out_stride, (int64_t)hq * head_dim, n_rows, true)))) return rc;
+    if (k_dev && ((rc = check_rows("k_dev", dtype, k_dev, k_stride, (int64_t)hk * head_dim, n_rows, false)) ||
+                  (rc = check_rows("k_out_dev", dtype, k_out_dev, k_out_stride, (int64_t)hk * head_dim, n_rows, true)))) return rc;
+    const QkRows r{q_dev, k_dev, nullptr, q_stride, k_stride, 0, q_out_dev, k_out_dev, q_out_stride, k_out_stride, pos_dev, nullptr, n_rows, hq, hk, head_dim};
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (dtype == SJD_DTYPE_F32) launch_qk_rope<float>(o, r, s);
+    else if (dtype == SJD_DTYPE_BF16) launch_qk_rope<bf16>(o, r, s);
+    else launch_qk_rope<f16>(o, r, s);
+    HIP_TRY(hipGetLastError());
+    return SJD_OK;
+}
+
+int sjd_op_kv4_write(const sjd_kv4 *cache, const int32_t *slot_dev, const void *k_dev, int64_t k_stride, const void *v_dev,
+                     int64_t v_stride, int n_rows, const sjd_qk_opts *opts, const int32_t *pos_dev, const void *q_dev,
+                     int64_t q_stride, int n_heads, void *q_out_dev, int64_t q_out_stride, void *hip_stream) {
+    Kv4Cache c;
+    int rc = check_cache(cache, &c);
+    if (rc || (rc = check_work(n_rows, (int64_t)c.n_heads + (q_dev ? n_heads : 0), 32))) return rc;
+    const int64_t width = (int64_t)c.n_heads * c.dim;
+    QkOpts o;
+    if (opts) {
+        if ((rc = check_qk_opts(opts, pos_dev, c.dim, &o))) return rc;
+        if (width > 8192) return fail(SJD_EINVAL, "n_kv_heads * head_dim must not be over 8192 with opts");
+    } else if (q_dev) {
+        return fail(SJD_EINVAL, "queries need opts");
+    }
+    if (q_dev && (rc = check_heads(n_heads, c.n_heads))) return rc;
+    if (n_rows == 0) return SJD_OK;
+    if ((rc = check_pages(cache))) return rc;
+    if (!slot_dev) return fail(SJD_EINVAL, "null device pointer (slot_dev)");
+    if ((rc = check_rows("k_dev", cache->dtype, k_dev, k_stride, width, n_rows, false)) ||
+        (rc = check_rows("v_dev", cache->dtype, v_dev, v_stride, width, n_rows, false))) return rc;
+    if (q_dev && ((rc = check_rows("q_dev", cache->dtype, q_dev, q_stride, (int64_t)n_heads * c.dim, n_rows, false)) ||
+                  (rc = check_rows("q_out_dev", cache->dtype, q_out_dev, q_out_stride, (int64_t)n_heads * c.dim, n_rows, true)))) return rc;
+    const QkRows r{q_dev, k_dev, v_dev, q_stride, k_stride, v_stride, q_out_dev, nullptr, q_out_stride, 0, pos_dev, slot_dev, n_rows, q_dev ? n_heads : 0, c.n_heads, c.dim};
+    hipStream_t s = (hipStream_t)hip_stream;
+    const QkOpts *po = opts ? &o : nullptr;
+    if (cache->dtype == SJD_DTYPE_F32) launch_kv4_write<float>(c, po, r, s);
+    else if (cache->dtype == SJD_DTYPE_BF16) launch_kv4_write<bf16>(c, po, r, s);
+    else launch_kv4_write<f16>(c, po, r, s);
+    HIP_TRY(hipGetLastError());
+    return SJD_OK;
+}
+
+int sjd_op_kv4_read(const sjd_kv4 *cache, const int32_t *slot_dev, void *k_dev, int64_t k_stride, void *v_dev, int64_t v_stride,
+                    int n_rows, void *hip_stream) {
+    Kv4Cache c;
+    int rc = check_cache(cache, &c);
+    if (rc || (rc = check_work(n_rows, c.n_heads, 32))) return rc;
+    if (n_rows == 0) return SJD_OK;
+    const int64_t width = (int64_t)c.n_heads * c.dim;
+    if ((rc = check_pages(cache))) return rc;
+    if (!slot_dev) return fail(SJD_EINVAL, "null device pointer (slot_dev)");
+    if ((rc = check_rows("k_dev", cache->dtype, k_dev, k_stride, width, n_rows, true)) ||
+        (rc = check_rows("v_dev", cache->dtype, v_dev, v_stride, width, n_rows, true))) return rc;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (cache->dtype == SJD_DTYPE_F32) launch_kv4_read<float>(c, slot_dev, k_dev, k_stride, v_dev, v_stride, n_rows, s);
+    else if (cache->dtype == SJD_DTYPE_BF16) launch_kv4_read<bf16>(c, slot_dev, k_dev, k_stride, v_dev, v_stride, n_rows, s);
+    else launch_kv4_read<f16>(c, slot_dev, k_dev, k_stride, v_dev, v_stride, n_rows, s);
+    HIP_TRY(hipGetLastError());
+    return SJD_OK;
+}
+
+int sjd_kv4_attention_workspace(const sjd_kv4 *cache, const sjd_kv4_attention *args, size_t *bytes) {
+    if (!bytes) return fail(SJD_EINVAL, "null argument");
+    Kv4Attn a;
+    const int rc = check_attention(cache, args, &a);
+    if (rc) return rc;
+    *bytes = kv4_attention_workspace(a);
+    return SJD_OK;
+}
+
+int sjd_op_kv4_attention(const sjd_kv4 *cache, const sjd_kv4_attention *args, void *hip_stream) {
+    Kv4Attn a;
+    int rc = check_attention(cache, args, &a);
+    if (rc) return rc;
+    if (a.n_rows == 0 || a.n_seqs == 0 || a.max_q == 0) return SJD_OK;
+    if ((rc = check_pages(cache))) return rc;
+    const int64_t width = (int64_t)a.n_heads * a.cache.dim;
+    if ((rc = check_rows("q_dev", cache->dtype, a.q, a.q_stride, width, a.n_rows, false)) ||
+        (rc = check_rows("o_dev", cache->dtype, a.o, a.o_stride, width, a.n_rows, true))) return rc;
+    if (!a.kv_len || (!a.table && a.max_pages)) return fail(SJD_EINVAL, "null device pointer (kv_len_dev, page_table_dev)");
+    if (a.table_stride < 0) return fail(SJD_EINVAL, "table_stride must not be negative");
+    const size_t need = kv4_attention_workspace(a);
+    if (need && (!args->workspace_dev || args->workspace_bytes < need || (uintptr_t)args->workspace_dev % 16))
+        return fail(SJD_EINVAL, "this call needs %zu bytes of workspace on a 16-byte boundary", need);
+    a.partial = (float *)args->workspace_dev;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if (cache->dtype == SJD_DTYPE_F32) launch_kv4_attention<float>(a, s);
+    else if (cache->dtype == SJD_DTYPE_BF16) launch_kv4_attention<bf16>(a, s);
+    else launch_kv4_attention<f16>(a, s);
     HIP_TRY(hipGetLastError());
     return SJD_OK;
 }
