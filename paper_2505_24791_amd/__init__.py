@@ -113,7 +113,7 @@ def load_library() -> C.CDLL:
     lib.sjd_op_kv4_write.argtypes = [vp, vp, vp, C.c_int64, vp, C.c_int64, C.c_int, vp, vp, vp, C.c_int64, C.c_int, vp, C.c_int64, vp]
     lib.sjd_op_kv4_read.argtypes = [vp, vp, vp, C.c_int64, vp, C.c_int64, C.c_int, vp]
     lib.sjd_op_kv4_attention.argtypes = [vp, vp, vp]
-    lib.sjd_kv4_attention_workspace.argtypes = [vp, vp, C.POINTER(C.c_size_t)]
+    lib.sjd_kv4_attention_workspace.argtypes = [vp, vp, vp]
     lib.sjd_profile_enable.argtypes = [vp, C.c_uint32]
     lib.sjd_profile_read.argtypes = [vp, C.POINTER(SjdProfile), C.c_int]
     lib.sjd_flow_device_bytes.argtypes = [vp]
@@ -216,44 +216,63 @@ def op_attention_h16(qkv, n_samples, T, H):
 
 KV4_PAGE = 64          # tokens of a page of the 4-bit cache
 _NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
+_ROW_DTYPES = None     # torch types of rows -> DTYPE_* (torch is imported on first use)
 
 
 def _row_dtype(torch_dtype) -> int:
-    import torch
-    got = {torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}.get(torch_dtype)
-    _need(got is not None, f"rows must be float16, bfloat16 or float32, not {torch_dtype}")
-    return got
+    global _ROW_DTYPES
+    if _ROW_DTYPES is None:
+        import torch
+        _ROW_DTYPES = {torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+    code = _ROW_DTYPES.get(torch_dtype)
+    if code is None:
+        _refuse(f"rows must be float16, bfloat16 or float32, not {torch_dtype}")
+    return code
 
 
-def _need(ok, what: str) -> None:
-    if not ok:
-        raise SjdError(SJD_EINVAL, what)
+def _refuse(what: str):
+    raise SjdError(SJD_EINVAL, what)
 
 
-def _rows3(t, what: str, dtype, device):
-    """A tensor [rows, heads, head_dim] whose heads follow one another (any row stride)."""
-    _need(t.is_cuda and t.device == device and t.dtype == dtype, f"{what}: need a {dtype} tensor on {device}")
-    _need(t.dim() == 3, f"{what}: need [rows, heads, head_dim]")
-    n, h, d = t.shape
-    _need(n == 0 or ((d == 1 or t.stride(2) == 1) and (h == 1 or t.stride(1) == d)), f"{what}: the heads of a row must follow one another")
-    return t
+# The checks of the calls below run for every token of a serving loop: messages are made only where one fails.
+def _rows3(t, what: str, dtype, device: int):
+    """The shape of t [rows, heads, head_dim] (any row stride, the heads of a row following one another)."""
+    if t.dtype is not dtype or not t.is_cuda or t.get_device() != device or t.dim() != 3:
+        _refuse(f"{what}: need a {dtype} tensor [rows, heads, head_dim] on cuda:{device}")
+    shape = t.shape
+    n, h, d = shape
+    if n and not ((d == 1 or t.stride(2) == 1) and (h == 1 or t.stride(1) == d)):
+        _refuse(f"{what}: the heads of a row must follow one another")
+    return shape
 
 
-def _ints(t, what: str, shape, device):
-    import torch
-    _need(t.is_cuda and t.device == device and t.dtype == torch.int32 and t.is_contiguous() and tuple(t.shape) == tuple(shape),
-          f"{what}: need a contiguous int32 tensor {tuple(shape)} on {device}")
+def _ints(t, what: str, shape, device: int) -> int:
+    if t.dtype is not _int32() or not t.is_cuda or t.get_device() != device or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{what}: need a contiguous int32 tensor {tuple(shape)} on cuda:{device}")
     return t.data_ptr()
 
 
-def _launch(device, fn, *args) -> None:
+_I32 = None
+
+
+def _int32():
+    global _I32
+    if _I32 is None:
+        import torch
+        _I32 = torch.int32
+    return _I32
+
+
+def _launch(device: int, fn, *args) -> None:
     """Calls fn(*args, stream) with the tensors' device current, on that device's current stream."""
-    import torch
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+    from torch import cuda
+    if device == cuda.current_device():
+        rc = fn(*args, cuda.current_stream().cuda_stream)
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream().cuda_stream))
+        with cuda.device(device):
+            rc = fn(*args, cuda.current_stream().cuda_stream)
+    if rc:
+        _check(rc)
 
 
 class QkOpts:
@@ -266,48 +285,65 @@ class QkOpts:
     def __init__(self, *, norm: Optional[str] = "rms", eps: float = 1e-6, q_gain=None, q_shift=None, k_gain=None, k_shift=None,
                  rot_dim: int = 0, adjacent: bool = False, axis_pairs: Tuple[int, ...] = (), freq=None):
         import torch
-        _need(norm in _NORMS, f"norm must be one of {[n for n in _NORMS if n]}")
-        _need(rot_dim == 0 or (1 <= len(axis_pairs) <= 4 and freq is not None), "a rotation needs axis_pairs of 1 to 4 axes and freq")
-        self.tensors = {"q_gain": q_gain, "q_shift": q_shift, "k_gain": k_gain, "k_shift": k_shift, "freq": freq}
-        for name, t in self.tensors.items():
-            _need(t is None or (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 1),
-                  f"{name}: need a contiguous float32 vector on the GPU")
-        _need(freq is None or freq.numel() == rot_dim // 2, "freq: need rot_dim / 2 values")
+        if norm not in _NORMS:
+            _refuse(f"norm must be one of {[n for n in _NORMS if n]}")
+        if rot_dim and (not 1 <= len(axis_pairs) <= 4 or freq is None):
+            _refuse("a rotation needs axis_pairs of 1 to 4 axes and freq")
+        vectors = {"q_gain": q_gain, "q_shift": q_shift, "k_gain": k_gain, "k_shift": k_shift, "freq": freq}
+        self.tensors = [t for t in vectors.values() if t is not None]
+        for name, t in vectors.items():
+            if t is not None and not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 1):
+                _refuse(f"{name}: need a contiguous float32 vector on the GPU")
+        if freq is not None and freq.numel() != rot_dim // 2:
+            _refuse("freq: need rot_dim / 2 values")
+        sizes = {t.numel() for name, t in vectors.items() if t is not None and name != "freq"}
+        devices = {t.get_device() for t in self.tensors}
+        if len(sizes) > 1 or len(devices) > 1:
+            _refuse("gains and shifts need one size, and all vectors one device")
+        self.head_dim = sizes.pop() if sizes else None      # None: any
+        self.device = devices.pop() if devices else None
         self.n_axes = len(axis_pairs) if rot_dim else 0
         ptr = lambda t: t.data_ptr() if t is not None else None
         self.c = SjdQkOpts(_NORMS[norm], eps, ptr(q_gain), ptr(q_shift), ptr(k_gain), ptr(k_shift), rot_dim, 1 if adjacent else 0,
                            self.n_axes, (C.c_int32 * 4)(*axis_pairs[:4]), ptr(freq))
+        self.address = C.addressof(self.c)
 
-    def checked(self, head_dim: int, device):
+    def _for(self, head_dim: int, device: int) -> int:
         """The struct's address, for rows of this head size on this device."""
-        for name, t in self.tensors.items():
-            _need(t is None or (t.device == device and (name == "freq" or t.numel() == head_dim)), f"{name}: need {head_dim} values on {device}")
-        return C.addressof(self.c)
+        if (self.head_dim is not None and self.head_dim != head_dim) or (self.device is not None and self.device != device):
+            _refuse(f"the options hold vectors of {self.head_dim} values on cuda:{self.device}, the rows are of {head_dim} on cuda:{device}")
+        return self.address
 
 
 def op_qk_norm_rope(q, k, pos, opts: QkOpts, *, q_out=None, k_out=None):
     """``sjd_op_qk_norm_rope``: q [rows, heads, head_dim] and k [rows, kv_heads, head_dim] (either may be None; views of a fused projection's
     rows as they are), pos [rows, axes] int32 (None without a rotation).  Returns (q_out, k_out), new tensors unless given; an output
     may be its input."""
-    import torch
     some = q if q is not None else k
-    _need(some is not None, "need q or k")
-    dtype, device = some.dtype, some.device
+    if some is None:
+        _refuse("need q or k")
+    dtype, device = some.dtype, some.get_device()
     code = _row_dtype(dtype)
-    args = []
-    n, _, dim = _rows3(some, "q" if q is not None else "k", dtype, device).shape
-    for x, out, what in ((q, q_out, "q"), (k, k_out, "k")):
-        if x is None:
-            args.append((None, 0, 0, None, 0, None))
-            continue
-        _need(_rows3(x, what, dtype, device).shape[0] == n and x.shape[2] == dim, f"{what}: other rows or another head size than q")
-        if out is None:
-            out = torch.empty(x.shape, dtype=dtype, device=device)
-        _need(_rows3(out, what + "_out", dtype, device).shape == x.shape, f"{what}_out: need the shape of {what}")
-        args.append((x.data_ptr(), x.stride(0), x.shape[1], out.data_ptr(), out.stride(0), out))
-    (qp, qs, qh, qo, qos, q_out), (kp, ks, kh, ko, kos, k_out) = args
+    n, _, dim = _rows3(some, "q or k", dtype, device)
+    qp = qs = qh = qo = qos = kp = ks = kh = ko = kos = 0
+    if q is not None:
+        shape = q.shape
+        if q_out is None:
+            q_out = q.new_empty(shape)
+        elif _rows3(q_out, "q_out", dtype, device) != shape:
+            _refuse("q_out: need the shape of q")
+        qp, qs, qh, qo, qos = q.data_ptr(), q.stride(0), shape[1], q_out.data_ptr(), q_out.stride(0)
+    if k is not None:
+        shape = _rows3(k, "k", dtype, device)
+        if shape[0] != n or shape[2] != dim:
+            _refuse("k: other rows or another head size than q")
+        if k_out is None:
+            k_out = k.new_empty(shape)
+        elif _rows3(k_out, "k_out", dtype, device) != shape:
+            _refuse("k_out: need the shape of k")
+        kp, ks, kh, ko, kos = k.data_ptr(), k.stride(0), shape[1], k_out.data_ptr(), k_out.stride(0)
     p = _ints(pos, "pos", (n, opts.n_axes), device) if opts.n_axes else None
-    _launch(device, load_library().sjd_op_qk_norm_rope, code, opts.checked(dim, device), p, qp, qs, qh, kp, ks, kh, dim, qo, qos, ko, kos, n)
+    _launch(device, load_library().sjd_op_qk_norm_rope, code, opts._for(dim, device), p, qp, qs, qh, kp, ks, kh, dim, qo, qos, ko, kos, n)
     return q_out, k_out
 
 
@@ -317,9 +353,9 @@ class Kv4Cache:
 
     def __init__(self, pages, dtype):
         import torch
-        _need(pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous() and pages.dim() == 3 and pages.shape[2] % 68 == 0,
-              "pages: need a contiguous uint8 tensor [pages, kv_heads, 68 * head_dim] on the GPU")
-        self.pages, self.dtype, self.device = pages, dtype, pages.device
+        if not (pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous() and pages.dim() == 3 and pages.shape[2] % 68 == 0):
+            _refuse("pages: need a contiguous uint8 tensor [pages, kv_heads, 68 * head_dim] on the GPU")
+        self.pages, self.dtype, self.device = pages, dtype, pages.get_device()
         self.n_pages, self.kv_heads, self.head_dim = pages.shape[0], pages.shape[1], pages.shape[2] // 68
         self.c = SjdKv4(pages.data_ptr(), self.n_pages, self.kv_heads, self.head_dim, _row_dtype(dtype))
         self.address = C.addressof(self.c)
@@ -330,8 +366,8 @@ class Kv4Cache:
         return cls(torch.zeros((n_pages, kv_heads, 68 * head_dim), dtype=torch.uint8, device=device), dtype)
 
     def _kv(self, t, what: str, n: int):
-        _need(tuple(_rows3(t, what, self.dtype, self.device).shape) == (n, self.kv_heads, self.head_dim),
-              f"{what}: need [{n}, {self.kv_heads}, {self.head_dim}]")
+        if _rows3(t, what, self.dtype, self.device) != (n, self.kv_heads, self.head_dim):
+            _refuse(f"{what}: need [{n}, {self.kv_heads}, {self.head_dim}]")
         return t.data_ptr(), t.stride(0)
 
 
@@ -339,33 +375,39 @@ def op_kv4_write(cache: Kv4Cache, k, v, slot, *, opts: Optional[QkOpts] = None, 
     """``sjd_op_kv4_write``: rows k, v [rows, kv_heads, head_dim] become the tokens ``slot`` [rows] int32 (page * 64 + offset; -1: left out).
     With ``opts`` the keys are normed and rotated first, and with ``q`` [rows, heads, head_dim] the queries of those rows too: returns them
     (``q_out`` or a new tensor), else None."""
-    import torch
-    n = k.shape[0]
+    n, device, dim = k.shape[0], cache.device, cache.head_dim
     (kp, ks), (vp_, vs) = cache._kv(k, "k", n), cache._kv(v, "v", n)
-    sp = _ints(slot, "slot", (n,), cache.device)
+    sp = _ints(slot, "slot", (n,), device)
     op = pp = qp = qo = None
     qs = qos = heads = 0
     if opts is not None:
-        op = opts.checked(cache.head_dim, cache.device)
-        pp = _ints(pos, "pos", (n, opts.n_axes), cache.device) if opts.n_axes else None
+        op = opts._for(dim, device)
+        if opts.n_axes:
+            pp = _ints(pos, "pos", (n, opts.n_axes), device)
     if q is not None:
-        _need(opts is not None, "queries need opts")
-        _need(_rows3(q, "q", cache.dtype, cache.device).shape[0] == n and q.shape[2] == cache.head_dim, "q: other rows or another head size")
+        if opts is None:
+            _refuse("queries need opts")
+        shape = _rows3(q, "q", cache.dtype, device)
+        if shape[0] != n or shape[2] != dim:
+            _refuse("q: other rows or another head size")
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _need(_rows3(q_out, "q_out", cache.dtype, cache.device).shape == q.shape, "q_out: need the shape of q")
-        qp, qs, heads, qo, qos = q.data_ptr(), q.stride(0), q.shape[1], q_out.data_ptr(), q_out.stride(0)
-    _launch(cache.device, load_library().sjd_op_kv4_write, cache.address, sp, kp, ks, vp_, vs, n, op, pp, qp, qs, heads, qo, qos)
+            q_out = q.new_empty(shape)
+        elif _rows3(q_out, "q_out", cache.dtype, device) != shape:
+            _refuse("q_out: need the shape of q")
+        qp, qs, heads, qo, qos = q.data_ptr(), q.stride(0), shape[1], q_out.data_ptr(), q_out.stride(0)
+    _launch(device, load_library().sjd_op_kv4_write, cache.address, sp, kp, ks, vp_, vs, n, op, pp, qp, qs, heads, qo, qos)
     return q_out if q is not None else None
 
 
 def op_kv4_read(cache: Kv4Cache, slot, *, k_out=None, v_out=None):
     """``sjd_op_kv4_read``: the tokens ``slot`` [rows] int32 of the cache, (k, v) [rows, kv_heads, head_dim]; zeros for a slot outside it."""
-    import torch
     n = slot.shape[0]
     sp = _ints(slot, "slot", (n,), cache.device)
-    k_out, v_out = (torch.empty((n, cache.kv_heads, cache.head_dim), dtype=cache.dtype, device=cache.device) if t is None else t
-                    for t in (k_out, v_out))
+    shape = (n, cache.kv_heads, cache.head_dim)
+    if k_out is None:
+        k_out = cache.pages.new_empty(shape, dtype=cache.dtype)
+    if v_out is None:
+        v_out = cache.pages.new_empty(shape, dtype=cache.dtype)
     (kp, ks), (vp_, vs) = cache._kv(k_out, "k_out", n), cache._kv(v_out, "v_out", n)
     _launch(cache.device, load_library().sjd_op_kv4_read, cache.address, sp, kp, ks, vp_, vs, n)
     return k_out, v_out
@@ -377,29 +419,32 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
     page_table [seqs, max_pages] int32; sequence b has the rows q_start[b] .. q_start[b+1] - 1 (q_start [seqs + 1] int32; None: max_q
     each).  max_q and max_kv bound the rows and keys of a sequence (max_kv None: all that the table has room for).  Rows of no
     sequence are left as they are in ``out`` (None: a new tensor, which holds anything there)."""
-    import math
-    import torch
-    n, heads, dim = _rows3(q, "q", cache.dtype, cache.device).shape
-    _need(dim == cache.head_dim, "q: another head size than the cache's")
-    _need(page_table.dim() == 2 and kv_len.dim() == 1 and page_table.shape[0] == kv_len.shape[0], "need page_table [seqs, max_pages] and kv_len [seqs]")
+    device = cache.device
+    n, heads, dim = shape = _rows3(q, "q", cache.dtype, device)
+    if dim != cache.head_dim:
+        _refuse("q: another head size than the cache's")
+    if page_table.dim() != 2 or page_table.dtype is not _int32() or not page_table.is_cuda or page_table.get_device() != device \
+            or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        _refuse(f"page_table: need int32 rows [seqs, max_pages] on cuda:{device}")
     seqs, pages = page_table.shape
-    _need(page_table.is_cuda and page_table.device == cache.device and page_table.dtype == torch.int32 and (pages <= 1 or page_table.stride(1) == 1),
-          "page_table: need int32 rows on the cache's device")
+    lens = _ints(kv_len, "kv_len", (seqs,), device)
+    start = _ints(q_start, "q_start", (seqs + 1,), device) if q_start is not None else None
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    _need(_rows3(out, "out", cache.dtype, cache.device).shape == q.shape, "out: need the shape of q")
-    a = SjdKv4Attention(q.data_ptr(), out.data_ptr(), q.stride(0), out.stride(0), page_table.stride(0),
-                        _ints(q_start, "q_start", (seqs + 1,), cache.device) if q_start is not None else None,
-                        _ints(kv_len, "kv_len", (seqs,), cache.device), page_table.data_ptr(), seqs, heads, n, pages, max_q,
-                        pages * KV4_PAGE if max_kv is None else max_kv, 1 if causal else 0, skip_nearest, window,
-                        1.0 / math.sqrt(dim) if scale is None else scale, None, 0)
+        out = q.new_empty(shape)
+    elif _rows3(out, "out", cache.dtype, device) != shape:
+        _refuse("out: need the shape of q")
+    a = SjdKv4Attention(q.data_ptr(), out.data_ptr(), q.stride(0), out.stride(0), page_table.stride(0), start, lens, page_table.data_ptr(),
+                        seqs, heads, n, pages, max_q, pages * KV4_PAGE if max_kv is None else max_kv, 1 if causal else 0, skip_nearest,
+                        window, dim ** -0.5 if scale is None else scale, None, 0)
     lib = load_library()
-    need = C.c_size_t(0)
-    _check(lib.sjd_kv4_attention_workspace(cache.address, C.addressof(a), C.byref(need)))
+    address, need = C.addressof(a), C.c_size_t()
+    rc = lib.sjd_kv4_attention_workspace(cache.address, address, C.addressof(need))
+    if rc:
+        _check(rc)
     if need.value:
-        ws = torch.empty(need.value, dtype=torch.uint8, device=cache.device)
-        a.workspace, a.workspace_bytes = ws.data_ptr(), need.value
-    _launch(cache.device, lib.sjd_op_kv4_attention, cache.address, C.addressof(a))
+        workspace = cache.pages.new_empty(need.value)
+        a.workspace, a.workspace_bytes = workspace.data_ptr(), need.value
+    _launch(device, lib.sjd_op_kv4_attention, cache.address, address)
     return out
 
 

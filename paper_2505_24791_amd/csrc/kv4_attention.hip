@@ -7,6 +7,8 @@
 // type of the rows (float32 rows: every left operand as three bfloat16 pieces, which hold its 24 bits, on the same instruction).
 #include "kv4.h"
 
+#include <type_traits>
+
 namespace sjd {
 
 namespace {
@@ -88,8 +90,53 @@ __device__ __forceinline__ Tile tile_range(const Kv4Attn &a, const Seq &s, int r
     return t;
 }
 
+// A page as one lane holds it: per subtile of 16 tokens NG dwords of keys and NG of values, the scales of its key (one dword for the four
+// subtiles and each of its groups), and the value scales dealt over the 16 lanes that need the same ones.
+template <int NG> struct Page {
+    static constexpr int KS = NG > 4 ? NG / 4 : 1, VS = NG > 4 ? NG / 4 : 1;
+    u32 k[4][NG], v[4][NG], ks[KS], vs[VS];
+};
+template <int NG> __device__ __forceinline__ void load_dwords(u32 (&d)[NG], const uint8_t *p) {
+    typedef u32 vec __attribute__((ext_vector_type(NG == 1 ? 2 : NG > 4 ? 4 : NG)));
+    if constexpr (NG == 1) d[0] = *reinterpret_cast<const u32 *>(p);
+    else {
+        constexpr int W = NG > 4 ? 4 : NG;
+#pragma unroll
+        for (int i = 0; i < NG; i += W) {
+            const vec x = *reinterpret_cast<const vec *>(p + 4 * i);
+#pragma unroll
+            for (int e = 0; e < W; ++e) d[i + e] = x[e];
+        }
+    }
+}
+template <int NG> __device__ __forceinline__ void load_keys(Page<NG> &p, const uint8_t *blk, int r, int j) {
+    constexpr int DIM = 32 * NG;
+#pragma unroll
+    for (int i = 0; i < Page<NG>::KS; ++i) p.ks[i] = *reinterpret_cast<const u32 *>(blk + kv4_k_scale(DIM, r, j * NG / 4 + i));
+#pragma unroll
+    for (int t = 0; t < 4; ++t) load_dwords<NG>(p.k[t], blk + kv4_k_code(DIM, 16 * t + r, j * NG));
+}
+template <int NG> __device__ __forceinline__ void load_values(Page<NG> &p, const uint8_t *blk, int r, int j) {
+    constexpr int DIM = 32 * NG;
+#pragma unroll
+    for (int i = 0; i < Page<NG>::VS; ++i)
+        p.vs[i] = *reinterpret_cast<const u32 *>(blk + kv4_v_scale(DIM, 4 * j) + 4 * (min(r, 4 * NG - 1) + 16 * i));
+#pragma unroll
+    for (int t = 0; t < 4; ++t) load_dwords<NG>(p.v[t], blk + kv4_v_code(DIM, 16 * t + 4 * j, r));
+}
+// lane I of every 16
+template <int I> __device__ __forceinline__ u32 row_bcast(u32 x) {
+    return (u32)__builtin_amdgcn_update_dpp(0, (int)x, 0x150 + I, 0xf, 0xf, true);      // row_newbcast
+}
+template <int N, int I = 0, typename F> __device__ __forceinline__ void unroll(F &&f) {
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        unroll<N, I + 1>(f);
+    }
+}
+
 template <typename T, int NG>
-__global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Attn a, int n_tiles) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 || NG > 4 ? 2 : 3) void kv4_attention_kernel(Kv4Attn a, int n_tiles) {
     typedef typename Op<T>::t HT;
     typedef typename Half16<HT>::v8 v8;
     typedef T qv8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
@@ -97,7 +144,7 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Attn a, int n_til
     constexpr int RG = NG < 4 ? NG : 4, RDIM = 32 * RG, LD = RDIM + 4;      // groups joined at a time
     __shared__ __attribute__((aligned(16))) float acc[4][kRows * LD];
     __shared__ float ms[4][kRows], ls[4][kRows];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
     const int G = a.n_heads / a.cache.n_heads;
     const int part = blockIdx.x % a.n_splits, tile = blockIdx.x / a.n_splits % n_tiles, pair = blockIdx.x / a.n_splits / n_tiles;
     const int b = pair / a.cache.n_heads, h = pair % a.cache.n_heads;
@@ -112,6 +159,28 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Attn a, int n_til
     const int row = min(r0 + r, n_r - 1);
     int first, last;
     seen(a, sq, row / G, first, last);
+
+    // The wave's pages (every fourth of the piece): first those that every row sees whole, f0 .. f1 - 1, then the ones after and before.
+    const int f0 = min(max((tr.first_hi + kKv4Page - 1) / kKv4Page, p0), p1), f1 = max(min((tr.last_lo + 1) / kKv4Page, p1), f0);
+    auto mine = [&](int from) { return from + ((wave - (from - p0)) & 3); };           // the first of them from there on
+    auto count = [&](int from, int to) { return max(0, (to - mine(from) + 3) / 4); };
+    const int n_whole = count(f0, f1), n_after = count(f1, p1), n_pages = n_whole + n_after + count(p0, f0);
+    auto page_at = [&](int i) {
+        return i < n_whole ? mine(f0) + 4 * i : i < n_whole + n_after ? mine(f1) + 4 * (i - n_whole) : mine(p0) + 4 * (i - n_whole - n_after);
+    };
+    // the table's entry is fetched two pages ahead, the page one ahead
+    const int32_t *table = a.table + b * a.table_stride;
+    const uint8_t *base = a.cache.pages + (size_t)h * kv4_block_bytes(DIM);
+    const size_t page_bytes = (size_t)a.cache.n_heads * kv4_block_bytes(DIM);
+    auto entry = [&](int i) { return i < n_pages ? table[page_at(i)] : -1; };
+    auto valid = [&](int id) { return id >= 0 && id < a.cache.n_pages; };
+    auto block = [&](int id) { return base + (size_t)id * page_bytes; };
+    int id = entry(0), id_next = entry(1);
+    Page<NG> pg;
+    if (valid(id)) {
+        load_keys<NG>(pg, block(id), r, j);
+        load_values<NG>(pg, block(id), r, j);
+    }
 
     v8 qf[NG][NP];
     {
@@ -134,34 +203,35 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Attn a, int n_til
     for (int g = 0; g < NG; ++g) o[g][0] = o[g][1] = f32x4v{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;                 // of the row (m scaled, base 2); of the lane's tokens of the row
 
-    for (int page = p0 + wave; page < p1; page += 4) {
-        const int id = a.table[b * a.table_stride + page];
-        if (id < 0 || id >= a.cache.n_pages) continue;
-        const uint8_t *blk = a.cache.pages + ((size_t)id * a.cache.n_heads + h) * kv4_block_bytes(DIM);
+    // One page: scores, then the keys of the next page are requested; softmax; values, then those of the next page.
+    auto step = [&](auto masked_, int page) {
+        constexpr bool MASKED = decltype(masked_)::value;
         const int t0 = page * kKv4Page;
-        const bool full = t0 >= tr.first_hi && t0 + kKv4Page - 1 <= tr.last_lo;      // every row sees the whole page
-
+        const bool more = valid(id_next);
         f32x4v sc[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            sc[t] = f32x4v{0.f, 0.f, 0.f, 0.f};
-            const u32 *k = reinterpret_cast<const u32 *>(blk + kv4_k_code(DIM, 16 * t + r, j * NG));
+        for (int t = 0; t < 4; ++t) sc[t] = f32x4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int t = 0; t < 4; t += 2)
 #pragma unroll
             for (int s = 0; s < NG; ++s) {
-                const u32 ks = *reinterpret_cast<const u32 *>(blk + kv4_k_scale(DIM, r, (j * NG + s) / 4));
-                v8 kf;
-                decode8<HT>(k[s], pow2_byte(ks, t), kf);
 #pragma unroll
-                for (int c = 0; c < NP; ++c) sc[t] = Mfma16<HT>::run(kf, qf[s][c], sc[t]);
+                for (int u = t; u < t + 2; ++u) {
+                    v8 kf;
+                    decode8<HT>(pg.k[u][s], pow2_byte(pg.ks[s / 4], u), kf);
+#pragma unroll
+                    for (int c = 0; c < NP; ++c) sc[u] = Mfma16<HT>::run(kf, qf[s][c], sc[u]);
+                }
+                __builtin_amdgcn_sched_barrier(0);      // or all conversions of the page are begun at once, in as many registers
             }
-        }
+        if (more) load_keys<NG>(pg, block(id_next), r, j);
         float mx = -INFINITY;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int key = t0 + 16 * t + 4 * j + e;
-                if (!full && !(key >= first && key <= last)) sc[t][e] = -INFINITY;
+                if (MASKED) sc[t][e] = key >= first && key <= last ? sc[t][e] : -INFINITY;
                 mx = fmaxf(mx, sc[t][e]);
             }
         const float m_new = fmaxf(m, row_max(mx) * a.scale_log2);
@@ -177,9 +247,31 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Attn a, int n_til
                     for (int e = 0; e < 4; ++e) o[g][c][e] *= corr;
             m = m_new;
         }
-        bool nan_hidden = false;
+        // value scales as floats, byte k of a dword in vf[i][k], still dealt over the lanes
+        u32 sf[Page<NG>::VS][4];
+        constexpr u32 E = 0x7f800000u;
 #pragma unroll
-        for (int t = 0; t < 4; t += 2) {
+        for (int i = 0; i < Page<NG>::VS; ++i) {
+            sf[i][0] = (pg.vs[i] << 23) & E;
+            sf[i][1] = (pg.vs[i] << 15) & E;
+            sf[i][2] = (pg.vs[i] << 7) & E;
+            sf[i][3] = (pg.vs[i] >> 1) & E;
+        }
+        bool nan_hidden = false;
+        if (MASKED) {
+            // what no row sees is nothing's, and may be anything; a NaN that some row sees must not reach the others as 0 * NaN
+#pragma unroll
+            for (int i = 0; i < Page<NG>::VS; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int B = 4 * (min(r, 4 * NG - 1) + 16 * i) + k, key = t0 + 16 * (B / (4 * NG)) + 4 * j + B / NG % 4;
+                    const bool any = key >= lo && key <= hi, bad = sf[i][k] == E;
+                    nan_hidden |= any && bad;
+                    sf[i][k] = any && !bad ? sf[i][k] : 0u;
+                }
+        }
+        unroll<2>([&](auto half_) {
+            constexpr int t = 2 * decltype(half_)::value;
             v8 pf[NP];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -191,51 +283,52 @@ __global__ __launch_bounds__(256) void kv4_attention_kernel(Kv4Attn a, int n_til
                 for (int c = 0; c < NP; ++c) pf[c][e] = p[c];
             }
             if constexpr (NP == 1) l = Half16<HT>::add_all(pf[0], l);
-            u32 vw[2][NG], vs[2][NG];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const u32 *v = reinterpret_cast<const u32 *>(blk + kv4_v_code(DIM, 16 * (t + u) + 4 * j, r));
-                const u32 *s = reinterpret_cast<const u32 *>(blk + kv4_v_scale(DIM, 16 * (t + u) + 4 * j));
-#pragma unroll
-                for (int g = 0; g < NG; ++g) { vw[u][g] = v[g]; vs[u][g] = s[g]; }
-            }
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
+            unroll<NG>([&](auto g_) {
+                constexpr int g = decltype(g_)::value;
                 v8 vf[2];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int at = (e % 4) * NG + g;
-                    float s = pow2_byte(vs[e / 4][at / 4], at % 4);
-                    if (!full) {
-                        // what no row sees is nothing's, and may be anything; a NaN that some row sees must not reach the others as 0 * NaN
-                        const int key = t0 + 16 * (t + e / 4) + 4 * j + e % 4;
-                        if (!(key >= lo && key <= hi)) s = 0.f;
-                        else if (s == INFINITY) { s = 0.f; nan_hidden = true; }
-                    }
+                unroll<8>([&](auto e_) {
+                    constexpr int e = decltype(e_)::value;
+                    constexpr int at = (e % 4) * NG + g;                   // byte of the subtile's codes, and of its scales
+                    constexpr int tt = t + e / 4, B = tt * 4 * NG + at;
+                    const float s = __uint_as_float(row_bcast<(B / 4) % 16>(sf[B / 64][B % 4]));
                     HT x0, x1;
-                    const u32 w = vw[e / 4][at / 4];
-                    if (at % 4 == 0) decode2<HT, 0>(w, s, x0, x1);
-                    else if (at % 4 == 1) decode2<HT, 1>(w, s, x0, x1);
-                    else if (at % 4 == 2) decode2<HT, 2>(w, s, x0, x1);
-                    else decode2<HT, 3>(w, s, x0, x1);
+                    decode2<HT, at % 4>(pg.v[tt][at / 4], s, x0, x1);
                     vf[0][e] = x0;
                     vf[1][e] = x1;
-                }
+                });
 #pragma unroll
                 for (int c = 0; c < NP; ++c) {
                     o[g][0] = Mfma16<HT>::run(vf[0], pf[c], o[g][0]);
                     o[g][1] = Mfma16<HT>::run(vf[1], pf[c], o[g][1]);
                 }
-            }
-        }
-        if (!full && __builtin_amdgcn_ballot_w64(nan_hidden) != 0) {
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        });
+        if (more) load_values<NG>(pg, block(id_next), r, j);
+        if (MASKED && __builtin_amdgcn_ballot_w64(nan_hidden) != 0) {
+            const uint8_t *blk = block(id);
             for (int off = 0; off < kKv4Page; ++off)
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
                     if (t0 + off >= first && t0 + off <= last && blk[kv4_v_scale(DIM, off) + g] == 255)
                         o[g][0] = o[g][1] = f32x4v{NAN, NAN, NAN, NAN};
         }
-    }
+    };
+    auto walk = [&](auto masked_, int from, int to) {
+        for (int i = from; i < to; ++i) {
+            const int id_after = entry(i + 2);
+            if (valid(id)) {
+                step(masked_, page_at(i));
+            } else if (valid(id_next)) {          // this one is not seen, and the next not on its way yet
+                load_keys<NG>(pg, block(id_next), r, j);
+                load_values<NG>(pg, block(id_next), r, j);
+            }
+            id = id_next;
+            id_next = id_after;
+        }
+    };
+    walk(std::false_type{}, 0, n_whole);
+    walk(std::true_type{}, n_whole, n_pages);
     l = row_sum(l);
     if (j == 0) { ms[wave][r] = m; ls[wave][r] = l; }
 

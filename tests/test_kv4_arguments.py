@@ -113,13 +113,13 @@ def test_attention_that_is_refused(lib, kw, word):
 def test_attention_asks_for_its_workspace(lib):
     c, need = _cache(), C.c_size_t(0)
     a = _attn(max_pages=4000, max_kv=250000)
-    assert lib.sjd_kv4_attention_workspace(C.addressof(c), C.addressof(a), C.byref(need)) == sjd.SJD_OK and need.value > 0
+    assert lib.sjd_kv4_attention_workspace(C.addressof(c), C.addressof(a), C.addressof(need)) == sjd.SJD_OK and need.value > 0
     for ws, n in ((None, 0), (PTR, need.value - 1), (PTR + 4, need.value)):
         a.workspace, a.workspace_bytes = ws, n
         assert lib.sjd_op_kv4_attention(C.addressof(c), C.addressof(a), None) == sjd.SJD_EINVAL
         assert str(need.value) in lib.sjd_last_error().decode()
     short = _attn()
-    assert lib.sjd_kv4_attention_workspace(C.addressof(c), C.addressof(short), C.byref(need)) == sjd.SJD_OK and need.value == 0
+    assert lib.sjd_kv4_attention_workspace(C.addressof(c), C.addressof(short), C.addressof(need)) == sjd.SJD_OK and need.value == 0
     assert lib.sjd_kv4_attention_workspace(C.addressof(c), C.addressof(short), None) == sjd.SJD_EINVAL
 
 
