@@ -396,14 +396,31 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
     m = wave_max(m);
     const float mu = m == -INFINITY ? 0.f : m;
     float den = 0.f, sum[4] = {};
-    for (int s = s0; s < s1; ++s) {
-        const float *ps = p + (int64_t)s * (dim + 2);
-        const float w = __builtin_amdgcn_exp2f(ps[dim] - mu);
-        den = fmaf(w, ps[dim + 1], den);
+    for (int c0 = s0; c0 < s1; c0 += 64) {            // a lane a piece: its weight
+        const int n = min(64, s1 - c0);
+        const float *pc = p + (int64_t)c0 * (dim + 2);
+        float w = 0.f;
+        if (lane < n) {
+            w = __builtin_amdgcn_exp2f(pc[(int64_t)lane * (dim + 2) + dim] - mu);
+            den = fmaf(w, pc[(int64_t)lane * (dim + 2) + dim + 1], den);
+        }
+        for (int s = 0; s < n; s += 8) {              // eight pieces requested at a time
+            float x[8][4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (lane + 64 * c < dim) sum[c] = fmaf(w, ps[lane + 64 * c], sum[c]);
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    x[u][c] = s + u < n && lane + 64 * c < dim ? pc[(int64_t)(s + u) * (dim + 2) + lane + 64 * c] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float wu = __shfl(w, (s + u) & 63, 64);
+                if (s + u < n)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) sum[c] = fmaf(wu, x[u][c], sum[c]);
+            }
+        }
     }
+    den = wave_sum(den);
     T *out = (T *)a.o + at * a.o_stride + (int64_t)head * dim;
 #pragma unroll
     for (int c = 0; c < 4; ++c)

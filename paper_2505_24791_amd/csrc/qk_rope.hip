@@ -13,41 +13,56 @@ namespace sjd {
 
 namespace {
 
+// A constant of the polynomials below, in scalar registers: the compiler would keep all of them in vector registers around the loops.
+__device__ __forceinline__ double scalar(double x) {
+    asm("" : "+s"(x));
+    return x;
+}
+
 // cos and sin of p * f in float64.  The product of a 32-bit integer and a float32 needs 55 bits: taken as a sum of two doubles,
-// and so are the turns p f / 2 pi, of which the whole ones go; the fraction is good to 2^-52 of a turn.
+// and so are the turns p f / 2 pi, of which the whole ones go; the fraction is good to 2^-52 of a turn.  What is left after whole quarters, at
+// most pi / 4, goes into the Taylor sums up to x^15 and x^16 (the next terms are below 5e-17).
 __device__ __forceinline__ double2 unit(int32_t p, float f) {
 #pragma clang fp contract(off)   // th below is the rounded product, also where it is subtracted from
     const double ah = (double)p * (double)f, al = fma((double)p, (double)f, -ah);
-    const double ih = 0.15915494309189535, il = -9.839338337591243e-18;     // 1 / 2 pi
+    const double ih = 0.15915494309189535, il = -9.839338337591243e-18;      // 1 / 2 pi
     const double th = ah * ih, tl = fma(ah, ih, -th) + fma(ah, il, al * ih);
-    double s, c;
-    sincospi(2.0 * ((th - rint(th)) + tl), &s, &c);
-    return {c, s};
+    const double z = 4.0 * ((th - rint(th)) + tl), k = rint(z);
+    const double x = (z - k) * 1.5707963267948966, xx = x * x;
+    double s = scalar(-1.0 / 1307674368000), c = scalar(1.0 / 20922789888000);
+    s = fma(s, xx, scalar(1.0 / 6227020800));
+    c = fma(c, xx, scalar(-1.0 / 87178291200));
+    s = fma(s, xx, scalar(-1.0 / 39916800));
+    c = fma(c, xx, scalar(1.0 / 479001600));
+    s = fma(s, xx, scalar(1.0 / 362880));
+    c = fma(c, xx, scalar(-1.0 / 3628800));
+    s = fma(s, xx, scalar(-1.0 / 5040));
+    c = fma(c, xx, scalar(1.0 / 40320));
+    s = fma(s, xx, scalar(1.0 / 120));
+    c = fma(c, xx, scalar(-1.0 / 720));
+    s = fma(s, xx, scalar(-1.0 / 6));
+    c = fma(c, xx, scalar(1.0 / 24));
+    s = fma(s * xx, x, x);
+    c = fma(fma(c, xx, -0.5), xx, 1.0);
+    const int quarter = (int)k;
+    const double cc = quarter & 1 ? s : c, ss = quarter & 1 ? c : s;
+    return {(quarter + 1) & 2 ? -cc : cc, quarter & 2 ? -ss : ss};
 }
 
-// four values that start on a multiple of their own size
-template <typename T> __device__ __forceinline__ void load4(const T *p, float (&x)[4]) {
-    typedef T v4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    const v4 t = *reinterpret_cast<const v4 *>(p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = to_f32<T>(t[e]);
+template <int CTRL> __device__ __forceinline__ double dpp_add(double v) {
+    typedef int i32x2 __attribute__((ext_vector_type(2)));
+    const i32x2 x = __builtin_bit_cast(i32x2, v);
+    const i32x2 y = {__builtin_amdgcn_update_dpp(0, x.x, CTRL, 0xf, 0xf, true), __builtin_amdgcn_update_dpp(0, x.y, CTRL, 0xf, 0xf, true)};
+    return v + __builtin_bit_cast(double, y);
 }
-template <typename T> __device__ __forceinline__ void store4(T *p, const T (&x)[4]) {
-    typedef T v4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    *reinterpret_cast<v4 *>(p) = v4{x[0], x[1], x[2], x[3]};
-}
-
+// over L neighbouring lanes: quads by permutation, then mirrors (what they mirror is the same in all lanes of a part)
 template <int L> __device__ __forceinline__ double lanes_sum(double v) {
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    v = dpp_add<0xB1>(v);
+    v = dpp_add<0x4E>(v);
+    if constexpr (L >= 8) v = dpp_add<0x141>(v);
+    if constexpr (L >= 16) v = dpp_add<0x140>(v);
+    if constexpr (L >= 32) v += __shfl_xor(v, 16, 64);
     return v;
-}
-
-// Where a lane's two pieces of four channels begin: piece b holds the partners of piece a where the pairs are rot / 2 apart.
-struct Pieces { int a, b; };
-__device__ __forceinline__ Pieces pieces(int i, const QkOpts &o) {
-    if (!o.adjacent && 8 * i < o.rot) return {4 * i, 4 * i + o.rot / 2};
-    return {8 * i, 8 * i + 4};
 }
 
 __device__ __forceinline__ void turn(double &a, double &b, double2 u) {
@@ -56,55 +71,14 @@ __device__ __forceinline__ void turn(double &a, double &b, double2 u) {
     b = fma(b, u.x, x * u.y);
 }
 
-// One head of one row on L lanes (lane i of them): norm and rotation of the lane's eight channels.
-template <int L>
-__device__ __forceinline__ void head_turn(const QkOpts &o, int dim, int i, Pieces p, const float (&xa)[4], const float (&xb)[4],
-                                          const float *gain, const float *shift, const double2 *cs, double (&y)[8]) {
-    const bool live = 8 * i < dim;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        y[e] = live ? (double)xa[e] : 0.0;
-        y[4 + e] = live ? (double)xb[e] : 0.0;
-    }
-    if (o.norm) {
-        if (o.norm == 2) {
-            double s = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s += y[e];
-            const double mean = lanes_sum<L>(s) / dim;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = live ? y[e] - mean : 0.0;
-        }
-        double s = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s = fma(y[e], y[e], s);
-        const double r = rsqrt(lanes_sum<L>(s) / dim + (double)o.eps);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] *= r;
-        if (gain && live) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] *= (double)gain[p.a + e];
-                y[4 + e] *= (double)gain[p.b + e];
-            }
-        }
-        if (shift && live) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[e] += (double)shift[p.a + e];
-                y[4 + e] += (double)shift[p.b + e];
-            }
-        }
-    }
-    if (8 * i < o.rot) {
-        if (o.adjacent) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) turn(y[2 * e], y[2 * e + 1], cs[4 * i + e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) turn(y[e], y[4 + e], cs[4 * i + e]);
-        }
-    }
+// Through float32, kept apart: in one step the compiler rounds float64 to 16 bits with thirty instructions of its own.
+template <typename T> __device__ __forceinline__ T round_to(double x) { return from_f32<T>(keep_f32((float)x)); }
+
+// Where a lane's two pieces of four channels begin: piece b holds the partners of piece a where the pairs are rot / 2 apart.
+struct Pieces { int a, b; };
+__device__ __forceinline__ Pieces pieces(int i, const QkOpts &o) {
+    if (!o.adjacent && 8 * i < o.rot) return {4 * i, 4 * i + o.rot / 2};
+    return {8 * i, 8 * i + 4};
 }
 
 // ---- 4 bits ----------------------------------------------------------------------------------
@@ -131,16 +105,12 @@ __device__ __forceinline__ uint32_t encode8(const float (&x)[8], uint32_t byte) 
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], s, 2);
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], s, 3);
 }
-__device__ __forceinline__ uint32_t encode2(float a, float b, uint32_t byte) {
-    if (byte == 255) return 0;
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, a, b, scale_of(byte), 0) & 255u;
-}
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7fffffffu; }
 
-template <int L> __device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
-    return v;
+// the largest of four neighbouring lanes
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, true));
+    return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, true));
 }
 
 // Where a token's block is, nullptr where the slot is outside the cache.
@@ -149,139 +119,161 @@ __device__ __forceinline__ uint8_t *block_of(const Kv4Cache &c, int32_t slot, in
     return c.pages + ((size_t)(slot / kKv4Page) * c.n_heads + head) * kv4_block_bytes(c.dim);
 }
 
+// Eight channels (the ch-th eight) of a token's key or value for one head; four neighbouring lanes hold a group.  b == nullptr: nothing is stored.
+template <typename T, int N> struct Vec { typedef T v __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
+template <typename T> __device__ __forceinline__ void hold_key(uint8_t *b, int dim, int off, int ch, typename Vec<T, 8>::v r) {
+    float x[8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { x[e] = to_f32<T>(r[e]); top = max(top, mag(x[e])); }
+    const uint32_t sb = scale_byte<T>(quad_max(top));
+    if (!b) return;
+    *reinterpret_cast<uint32_t *>(b + kv4_k_code(dim, off, ch)) = encode8(x, sb);
+    if (ch % 4 == 0) b[kv4_k_scale(dim, off, ch / 4)] = (uint8_t)sb;
+}
+template <typename T> __device__ __forceinline__ void hold_value(uint8_t *b, int dim, int off, int ch, typename Vec<T, 8>::v r) {
+    float x[8];
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { x[e] = to_f32<T>(r[e]); top = max(top, mag(x[e])); }
+    const uint32_t sb = scale_byte<T>(quad_max(top));
+    if (!b) return;
+    const uint32_t w = encode8(x, sb);
+    uint8_t *d = b + kv4_v_code(dim, off, 4 * (ch % 4)) + ch / 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) d[e * (dim / 8)] = (uint8_t)(w >> (8 * e));        // the next pair is 4 NG bytes on
+    if (ch % 4 == 0) b[kv4_v_scale(dim, off) + ch / 4] = (uint8_t)sb;
+}
+
 // ---- kernels ---------------------------------------------------------------------------------
 
 constexpr int kThreads = 256;
 
-// A workgroup takes `per` rows.  First every (row, pair) gets its cos and sin, once for all heads; then L lanes a head, all heads of its
-// rows.  WRITE: keys go to LDS, rounded to their type, instead of memory, and with the values from there into the cache.
+// A workgroup takes `per` rows: cos and sin of every (row, pair) once for all heads, through LDS, then L lanes a head, eight channels each, the
+// next head's row requested under the present one's arithmetic.  WRITE: rounded keys go to LDS instead of memory, and with the values from
+// there into the cache.
+struct RopeShape { int per; uint32_t magic; double per_dim; };      // magic: n / heads = n * magic >> 32 for the n of a workgroup
+
 template <typename T, int L, bool WRITE>
-__global__ __launch_bounds__(kThreads) void qk_rope_kernel(QkOpts o, QkRows r, Kv4Cache c, int per) {
-    extern __shared__ char smem[];
-    double2 *cs = reinterpret_cast<double2 *>(smem);
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kernel(QkOpts o, QkRows r, Kv4Cache c, RopeShape sh) {
+    typedef typename Vec<T, 4>::v v4;
+    typedef typename Vec<T, 8>::v v8;
+    constexpr int SLOTS = kThreads / L;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
     const int pairs = o.rot / 2;
-    T *keys = reinterpret_cast<T *>(smem + (size_t)per * pairs * sizeof(double2));      // [per][n_kv][dim]
-    const int row0 = blockIdx.x * per, rows = min(per, r.n_rows - row0);
-    const int tid = threadIdx.x;
+    double2 *cs = reinterpret_cast<double2 *>(smem);                                     // [per][pairs]
+    float *affine = reinterpret_cast<float *>(smem + (size_t)sh.per * pairs * sizeof(double2));   // [4][dim] gains of q and k, shifts of q and k
+    T *keys = reinterpret_cast<T *>(affine + 4 * r.dim);                                 // [per][n_kv][dim]
+    const int tid = threadIdx.x, i = tid % L, row0 = blockIdx.x * sh.per, rows = min(sh.per, r.n_rows - row0);
+    const int n_q = r.q ? r.n_heads : 0, heads = n_q + (r.k ? r.n_kv : 0), n = rows * heads;
+    const Pieces p = pieces(i, o);
+    const bool live = 8 * i < r.dim, turns = 8 * i < o.rot;
+    v4 xa, xb;
+    auto split = [&](int t, int &row, int &h) {
+        row = heads == 1 ? t : (int)__umulhi((uint32_t)t, sh.magic);
+        h = t - row * heads;
+    };
+    auto fetch = [&](int t) {
+        if (t >= n || !live) return;
+        int row, h;
+        split(t, row, h);
+        const T *x = h < n_q ? (const T *)r.q + (row0 + row) * r.q_stride + h * r.dim : (const T *)r.k + (row0 + row) * r.k_stride + (h - n_q) * r.dim;
+        xa = *reinterpret_cast<const v4 *>(x + p.a);
+        xb = *reinterpret_cast<const v4 *>(x + p.b);
+    };
+    fetch(tid / L);
+    if (o.norm)
+        for (int e = tid; e < r.dim; e += kThreads) {
+            affine[e] = o.q_gain ? o.q_gain[e] : 1.f;
+            affine[r.dim + e] = o.k_gain ? o.k_gain[e] : 1.f;
+            affine[2 * r.dim + e] = o.q_shift ? o.q_shift[e] : 0.f;
+            affine[3 * r.dim + e] = o.k_shift ? o.k_shift[e] : 0.f;
+        }
     for (int t = tid; t < rows * pairs; t += kThreads) {
-        const int row = t / pairs, i = t - row * pairs;
+        const int row = t / pairs, pi = t - row * pairs;
         int axis = 0;
-        while (axis + 1 < o.n_axes && i >= o.axis_end[axis]) ++axis;
-        cs[t] = unit(r.pos[(int64_t)(row0 + row) * o.n_axes + axis], o.freq[i]);
+        while (axis + 1 < o.n_axes && pi >= o.axis_end[axis]) ++axis;
+        cs[t] = unit(r.pos[(int64_t)(row0 + row) * o.n_axes + axis], o.freq[pi]);
     }
     __syncthreads();
-    const int i = tid % L, heads = (r.q ? r.n_heads : 0) + (r.k ? r.n_kv : 0);
-    const Pieces p = pieces(i, o);
-    const bool live = 8 * i < r.dim;
-    for (int t = tid / L; t < rows * heads; t += kThreads / L) {
-        const int row = t / heads, hh = t - row * heads;
-        const bool is_q = r.q && hh < r.n_heads;
-        const int h = is_q ? hh : hh - (r.q ? r.n_heads : 0);
-        const int64_t at = row0 + row;
-        const T *x = is_q ? (const T *)r.q + at * r.q_stride + (int64_t)h * r.dim : (const T *)r.k + at * r.k_stride + (int64_t)h * r.dim;
-        float xa[4] = {}, xb[4] = {};
-        if (live) {
-            load4<T>(x + p.a, xa);
-            load4<T>(x + p.b, xb);
-        }
+    for (int t = tid / L; t < n; t += SLOTS) {
+        int row, h;
+        split(t, row, h);
+        const bool is_q = h < n_q;
         double y[8];
-        head_turn<L>(o, r.dim, i, p, xa, xb, is_q ? o.q_gain : o.k_gain, is_q ? o.q_shift : o.k_shift, cs + row * pairs, y);
-        if (!live) continue;
-        T ya[4], yb[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            ya[e] = from_f32<T>((float)y[e]);
-            yb[e] = from_f32<T>((float)y[4 + e]);
+            y[e] = live ? (double)to_f32<T>(xa[e]) : 0.0;
+            y[4 + e] = live ? (double)to_f32<T>(xb[e]) : 0.0;
         }
-        if (WRITE && !is_q) {
-            T *k = keys + ((size_t)row * r.n_kv + h) * r.dim;
-            store4<T>(k + p.a, ya);
-            store4<T>(k + p.b, yb);
-        } else {
-            T *out = is_q ? (T *)r.q_out + at * r.q_out_stride + (int64_t)h * r.dim : (T *)r.k_out + at * r.k_out_stride + (int64_t)h * r.dim;
-            store4<T>(out + p.a, ya);
-            store4<T>(out + p.b, yb);
+        fetch(t + SLOTS);
+        if (o.norm) {
+            if (o.norm == 2) {
+                double s = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s += y[e];
+                const double mean = lanes_sum<L>(s) * sh.per_dim;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = live ? y[e] - mean : 0.0;
+            }
+            double s = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s = fma(y[e], y[e], s);
+            const double n_inv = rsqrt(fma(lanes_sum<L>(s), sh.per_dim, (double)o.eps));
+            const float *g = affine + (is_q ? 0 : r.dim);
+            if (live) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = fma(y[e] * n_inv, (double)g[p.a + e], (double)g[2 * r.dim + p.a + e]);
+                    y[4 + e] = fma(y[4 + e] * n_inv, (double)g[p.b + e], (double)g[2 * r.dim + p.b + e]);
+                }
+            }
         }
+        if (!live) continue;
+        if (turns) {
+            const double2 *u = cs + row * pairs + 4 * i;
+            if (o.adjacent) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) turn(y[2 * e], y[2 * e + 1], u[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) turn(y[e], y[4 + e], u[e]);
+            }
+        }
+        T *out = is_q ? (T *)r.q_out + (row0 + row) * r.q_out_stride + h * r.dim
+               : WRITE ? keys + ((size_t)row * r.n_kv + h - n_q) * r.dim : (T *)r.k_out + (row0 + row) * r.k_out_stride + (h - n_q) * r.dim;
+        *reinterpret_cast<v4 *>(out + p.a) = v4{round_to<T>(y[0]), round_to<T>(y[1]), round_to<T>(y[2]), round_to<T>(y[3])};
+        *reinterpret_cast<v4 *>(out + p.b) = v4{round_to<T>(y[4]), round_to<T>(y[5]), round_to<T>(y[6]), round_to<T>(y[7])};
     }
     if constexpr (WRITE) {
         __syncthreads();
-        const int ng = r.dim / 32, chunks = r.dim / 8;
-        // keys: eight channels a lane, four lanes a group (their number is a multiple of four: a group's lanes stay together)
-        for (int t = tid; t < rows * r.n_kv * chunks; t += kThreads) {
-            const int row = t / (r.n_kv * chunks), rest = t - row * r.n_kv * chunks, h = rest / chunks, ch = rest - h * chunks;
-            float x[8];
-            const T *k = keys + ((size_t)row * r.n_kv + h) * r.dim + 8 * ch;
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) { x[e] = to_f32<T>(k[e]); top = max(top, mag(x[e])); }
-            top = lanes_max<4>(top);
+        for (int t = tid / L; t < rows * r.n_kv; t += SLOTS) {
+            const int row = t / r.n_kv, h = t - row * r.n_kv;
+            const v8 v = *reinterpret_cast<const v8 *>((const T *)r.v + (row0 + row) * r.v_stride + h * r.dim + 8 * i);
             const int32_t slot = r.slot[row0 + row];
             uint8_t *b = block_of(c, slot, h);
-            if (!b) continue;
-            const int off = slot % kKv4Page;
-            const uint32_t sb = scale_byte<T>(top);
-            *reinterpret_cast<uint32_t *>(b + kv4_k_code(r.dim, off, ch)) = encode8(x, sb);
-            if (ch % 4 == 0) b[kv4_k_scale(r.dim, off, ch / 4)] = (uint8_t)sb;
-        }
-        // values: sixteen lanes a token and head, a channel pair of each group
-        for (int t = tid; t < rows * r.n_kv * 16; t += kThreads) {
-            const int row = t / (r.n_kv * 16), rest = t - row * r.n_kv * 16, h = rest / 16, n = rest % 16;
-            const int32_t slot = r.slot[row0 + row];
-            uint8_t *b = block_of(c, slot, h);
-            const int off = slot % kKv4Page;
-            const T *v = (const T *)r.v + (int64_t)(row0 + row) * r.v_stride + (int64_t)h * r.dim + 2 * n;
-            for (int g = 0; g < ng; ++g) {
-                const float x0 = to_f32<T>(v[32 * g]), x1 = to_f32<T>(v[32 * g + 1]);
-                const uint32_t sb = scale_byte<T>(lanes_max<16>(max(mag(x0), mag(x1))));
-                if (!b) continue;
-                b[kv4_v_code(r.dim, off, n) + g] = (uint8_t)encode2(x0, x1, sb);
-                if (n == 0) b[kv4_v_scale(r.dim, off) + g] = (uint8_t)sb;
-            }
+            const int off = slot & (kKv4Page - 1);
+            hold_key<T>(b, r.dim, off, i, *reinterpret_cast<const v8 *>(keys + (size_t)t * r.dim + 8 * i));
+            hold_value<T>(b, r.dim, off, i, v);
         }
     }
 }
 
-// keys and values as they are
+// keys and values as they are: eight channels of a token's key and value for one head a thread
 template <typename T>
 __global__ __launch_bounds__(kThreads) void kv4_write_kernel(QkRows r, Kv4Cache c) {
-    const int ng = r.dim / 32, chunks = r.dim / 8;
+    typedef typename Vec<T, 8>::v v8;
+    const int chunks = r.dim / 8;
     const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t n_k = (int64_t)r.n_rows * r.n_kv * chunks;
-    const int64_t k_blocks = (n_k + kThreads - 1) / kThreads * kThreads;
-    if (id < k_blocks) {
-        if (id >= n_k) return;
-        const int64_t row = id / (r.n_kv * chunks);
-        const int rest = (int)(id - row * r.n_kv * chunks), h = rest / chunks, ch = rest - h * chunks;
-        const T *k = (const T *)r.k + row * r.k_stride + (int64_t)h * r.dim + 8 * ch;
-        float x[8];
-        uint32_t top = 0;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { x[e] = to_f32<T>(k[e]); top = max(top, mag(x[e])); }
-        top = lanes_max<4>(top);
-        const int32_t slot = r.slot[row];
-        uint8_t *b = block_of(c, slot, h);
-        if (!b) return;
-        const int off = slot % kKv4Page;
-        const uint32_t sb = scale_byte<T>(top);
-        *reinterpret_cast<uint32_t *>(b + kv4_k_code(r.dim, off, ch)) = encode8(x, sb);
-        if (ch % 4 == 0) b[kv4_k_scale(r.dim, off, ch / 4)] = (uint8_t)sb;
-        return;
-    }
-    const int64_t t = id - k_blocks;
-    if (t >= (int64_t)r.n_rows * r.n_kv * 16) return;
-    const int64_t row = t / (r.n_kv * 16);
-    const int rest = (int)(t - row * r.n_kv * 16), h = rest / 16, n = rest % 16;
+    const int64_t row = id / (r.n_kv * chunks);
+    if (row >= r.n_rows) return;
+    const int rest = (int)(id - row * r.n_kv * chunks), h = rest / chunks, ch = rest - h * chunks;
+    const v8 k = *reinterpret_cast<const v8 *>((const T *)r.k + row * r.k_stride + (int64_t)h * r.dim + 8 * ch);
+    const v8 v = *reinterpret_cast<const v8 *>((const T *)r.v + row * r.v_stride + (int64_t)h * r.dim + 8 * ch);
     const int32_t slot = r.slot[row];
     uint8_t *b = block_of(c, slot, h);
-    const int off = slot % kKv4Page;
-    const T *v = (const T *)r.v + row * r.v_stride + (int64_t)h * r.dim + 2 * n;
-    for (int g = 0; g < ng; ++g) {
-        const float x0 = to_f32<T>(v[32 * g]), x1 = to_f32<T>(v[32 * g + 1]);
-        const uint32_t sb = scale_byte<T>(lanes_max<16>(max(mag(x0), mag(x1))));
-        if (!b) continue;
-        b[kv4_v_code(r.dim, off, n) + g] = (uint8_t)encode2(x0, x1, sb);
-        if (n == 0) b[kv4_v_scale(r.dim, off) + g] = (uint8_t)sb;
-    }
+    hold_key<T>(b, r.dim, slot & (kKv4Page - 1), ch, k);
+    hold_value<T>(b, r.dim, slot & (kKv4Page - 1), ch, v);
 }
 
 // eight channels a lane: of the keys of a token, then of its values; zeros for a slot outside the cache
@@ -318,16 +310,28 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4Cache c, const in
     }
 }
 
+template <typename T, int L, bool WRITE>
+void launch_rope_lanes(const QkOpts &o, QkRows r, const Kv4Cache &c, hipStream_t s) {
+    if (!r.q) r.n_heads = 0;
+    if (!r.k) r.n_kv = 0;
+    constexpr int GROUPS = kThreads / L;
+    const int heads = r.n_heads + r.n_kv;
+    // Rows of a workgroup: eight heads for a lane group, but 1024 workgroups where there are rows enough, and LDS that lets six share a CU
+    const size_t row_lds = (size_t)(o.rot / 2) * sizeof(double2) + (WRITE ? (size_t)r.n_kv * r.dim * sizeof(T) : 0), affine = 4 * r.dim * sizeof(float);
+    int per = 8 * GROUPS / heads;
+    if (per > r.n_rows / 1024) per = r.n_rows / 1024;
+    while (per > 1 && per * row_lds + affine > 26624) per /= 2;
+    if (per < 1) per = 1;
+    const RopeShape sh{per, heads > 1 ? (uint32_t)(((1ull << 32) + heads - 1) / heads) : 0u, 1.0 / r.dim};
+    hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE>), dim3((r.n_rows + per - 1) / per), dim3(kThreads), per * row_lds + affine, s, o, r, c, sh);
+}
+
 template <typename T, bool WRITE>
 void launch_rope(const QkOpts &o, const QkRows &r, const Kv4Cache &c, hipStream_t s) {
-    const size_t row_lds = (size_t)(o.rot / 2) * sizeof(double2) + (WRITE ? (size_t)r.n_kv * r.dim * sizeof(T) : 0);
-    const int per = r.n_rows >= 4096 && 4 * row_lds <= 32768 ? 4 : 1;
-    const size_t lds = per * row_lds;
-    const dim3 grid((r.n_rows + per - 1) / per);
-    if (r.dim <= 32) hipLaunchKernelGGL((qk_rope_kernel<T, 4, WRITE>), grid, dim3(kThreads), lds, s, o, r, c, per);
-    else if (r.dim <= 64) hipLaunchKernelGGL((qk_rope_kernel<T, 8, WRITE>), grid, dim3(kThreads), lds, s, o, r, c, per);
-    else if (r.dim <= 128) hipLaunchKernelGGL((qk_rope_kernel<T, 16, WRITE>), grid, dim3(kThreads), lds, s, o, r, c, per);
-    else hipLaunchKernelGGL((qk_rope_kernel<T, 32, WRITE>), grid, dim3(kThreads), lds, s, o, r, c, per);
+    if (r.dim <= 32) launch_rope_lanes<T, 4, WRITE>(o, r, c, s);
+    else if (r.dim <= 64) launch_rope_lanes<T, 8, WRITE>(o, r, c, s);
+    else if (r.dim <= 128) launch_rope_lanes<T, 16, WRITE>(o, r, c, s);
+    else launch_rope_lanes<T, 32, WRITE>(o, r, c, s);
 }
 
 }  // namespace
@@ -339,9 +343,8 @@ template <typename T> void launch_qk_rope(const QkOpts &o, const QkRows &r, hipS
 template <typename T> void launch_kv4_write(const Kv4Cache &c, const QkOpts *o, const QkRows &r, hipStream_t s) {
     if (r.n_rows <= 0) return;
     if (o) return launch_rope<T, true>(*o, r, c, s);
-    const int64_t nk = ((int64_t)r.n_rows * r.n_kv * (r.dim / 8) + kThreads - 1) / kThreads;
-    const int64_t nv = ((int64_t)r.n_rows * r.n_kv * 16 + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL((kv4_write_kernel<T>), dim3((unsigned)(nk + nv)), dim3(kThreads), 0, s, r, c);
+    const int64_t n = ((int64_t)r.n_rows * r.n_kv * (r.dim / 8) + kThreads - 1) / kThreads;
+    hipLaunchKernelGGL((kv4_write_kernel<T>), dim3((unsigned)n), dim3(kThreads), 0, s, r, c);
 }
 
 template <typename T> void launch_kv4_read(const Kv4Cache &c, const int32_t *slot, void *k, int64_t k_stride, void *v, int64_t v_stride,
