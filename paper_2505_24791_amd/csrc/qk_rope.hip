@@ -161,14 +161,14 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kern
     constexpr int SLOTS = kThreads / L;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int pairs = o.rot / 2;
-    double2 *cs = reinterpret_cast<double2 *>(smem);                                     // [per][pairs]
+    double2 *cs = reinterpret_cast<double2 *>(smem);                                     // [per][4][pairs / 4]: a lane's four pairs apart, or neighbouring lanes meet in a bank
     float *affine = reinterpret_cast<float *>(smem + (size_t)sh.per * pairs * sizeof(double2));   // [4][dim] gains of q and k, shifts of q and k
     T *keys = reinterpret_cast<T *>(affine + 4 * r.dim);                                 // [per][n_kv][dim]
     const int tid = threadIdx.x, i = tid % L, row0 = blockIdx.x * sh.per, rows = min(sh.per, r.n_rows - row0);
     const int n_q = r.q ? r.n_heads : 0, heads = n_q + (r.k ? r.n_kv : 0), n = rows * heads;
     const Pieces p = pieces(i, o);
-    const bool live = 8 * i < r.dim, turns = 8 * i < o.rot;
-    v4 xa, xb;
+    const bool live = 8 * i < r.dim, turns = 8 * i < o.rot, shifted = o.q_shift || o.k_shift;
+    v4 xa = {}, xb = {};                       // lanes past the head keep zeros
     auto split = [&](int t, int &row, int &h) {
         row = heads == 1 ? t : (int)__umulhi((uint32_t)t, sh.magic);
         h = t - row * heads;
@@ -193,7 +193,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kern
         const int row = t / pairs, pi = t - row * pairs;
         int axis = 0;
         while (axis + 1 < o.n_axes && pi >= o.axis_end[axis]) ++axis;
-        cs[t] = unit(r.pos[(int64_t)(row0 + row) * o.n_axes + axis], o.freq[pi]);
+        cs[row * pairs + (pi & 3) * (pairs / 4) + pi / 4] = unit(r.pos[(int64_t)(row0 + row) * o.n_axes + axis], o.freq[pi]);
     }
     __syncthreads();
     for (int t = tid / L; t < n; t += SLOTS) {
@@ -203,8 +203,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kern
         double y[8];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            y[e] = live ? (double)to_f32<T>(xa[e]) : 0.0;
-            y[4 + e] = live ? (double)to_f32<T>(xb[e]) : 0.0;
+            y[e] = (double)to_f32<T>(xa[e]);
+            y[4 + e] = (double)to_f32<T>(xb[e]);
         }
         fetch(t + SLOTS);
         if (o.norm) {
@@ -222,22 +222,31 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kern
             const double n_inv = rsqrt(fma(lanes_sum<L>(s), sh.per_dim, (double)o.eps));
             const float *g = affine + (is_q ? 0 : r.dim);
             if (live) {
+                const f32x4 ga = *reinterpret_cast<const f32x4 *>(g + p.a), gb = *reinterpret_cast<const f32x4 *>(g + p.b);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    y[e] = fma(y[e] * n_inv, (double)g[p.a + e], (double)g[2 * r.dim + p.a + e]);
-                    y[4 + e] = fma(y[4 + e] * n_inv, (double)g[p.b + e], (double)g[2 * r.dim + p.b + e]);
+                    y[e] *= n_inv * (double)ga[e];
+                    y[4 + e] *= n_inv * (double)gb[e];
+                }
+                if (shifted) {
+                    const f32x4 sa = *reinterpret_cast<const f32x4 *>(g + 2 * r.dim + p.a), sb = *reinterpret_cast<const f32x4 *>(g + 2 * r.dim + p.b);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        y[e] += (double)sa[e];
+                        y[4 + e] += (double)sb[e];
+                    }
                 }
             }
         }
         if (!live) continue;
         if (turns) {
-            const double2 *u = cs + row * pairs + 4 * i;
+            const double2 *u = cs + row * pairs + i;
             if (o.adjacent) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) turn(y[2 * e], y[2 * e + 1], u[e]);
+                for (int e = 0; e < 4; ++e) turn(y[2 * e], y[2 * e + 1], u[e * (pairs / 4)]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) turn(y[e], y[4 + e], u[e]);
+                for (int e = 0; e < 4; ++e) turn(y[e], y[4 + e], u[e * (pairs / 4)]);
             }
         }
         T *out = is_q ? (T *)r.q_out + (row0 + row) * r.q_out_stride + h * r.dim
@@ -246,16 +255,30 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kern
         *reinterpret_cast<v4 *>(out + p.b) = v4{round_to<T>(y[4]), round_to<T>(y[5]), round_to<T>(y[6]), round_to<T>(y[7])};
     }
     if constexpr (WRITE) {
-        __syncthreads();
-        for (int t = tid / L; t < rows * r.n_kv; t += SLOTS) {
+        constexpr int AHEAD = 4;                            // values requested before the first is needed
+        const int n_v = rows * r.n_kv;
+        v8 xv[AHEAD];
+        auto fetch_v = [&](int u, int t) {
+            if (t >= n_v) return;
             const int row = t / r.n_kv, h = t - row * r.n_kv;
-            const v8 v = *reinterpret_cast<const v8 *>((const T *)r.v + (row0 + row) * r.v_stride + h * r.dim + 8 * i);
-            const int32_t slot = r.slot[row0 + row];
-            uint8_t *b = block_of(c, slot, h);
-            const int off = slot & (kKv4Page - 1);
-            hold_key<T>(b, r.dim, off, i, *reinterpret_cast<const v8 *>(keys + (size_t)t * r.dim + 8 * i));
-            hold_value<T>(b, r.dim, off, i, v);
-        }
+            xv[u] = *reinterpret_cast<const v8 *>((const T *)r.v + (row0 + row) * r.v_stride + h * r.dim + 8 * i);
+        };
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) fetch_v(u, tid / L + u * SLOTS);
+        __syncthreads();
+        for (int t0 = tid / L; t0 < n_v; t0 += AHEAD * SLOTS)
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int t = t0 + u * SLOTS;
+                if (t >= n_v) break;
+                const int row = t / r.n_kv, h = t - row * r.n_kv;
+                const int32_t slot = r.slot[row0 + row];
+                uint8_t *b = block_of(c, slot, h);
+                const int off = slot & (kKv4Page - 1);
+                hold_value<T>(b, r.dim, off, i, xv[u]);
+                fetch_v(u, t + AHEAD * SLOTS);
+                hold_key<T>(b, r.dim, off, i, *reinterpret_cast<const v8 *>(keys + (size_t)t * r.dim + 8 * i));
+            }
     }
 }
 
