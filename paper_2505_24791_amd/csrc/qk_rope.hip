@@ -71,8 +71,17 @@ __device__ __forceinline__ void turn(double &a, double &b, double2 u) {
     b = fma(b, u.x, x * u.y);
 }
 
+// N values that start on a multiple of their own size
+template <typename T, int N> struct Vec { typedef T v __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
+
 // Through float32, kept apart: in one step the compiler rounds float64 to 16 bits with thirty instructions of its own.
-template <typename T> __device__ __forceinline__ T round_to(double x) { return from_f32<T>(keep_f32((float)x)); }
+template <typename T> __device__ __forceinline__ void store4(T *p, const double *y) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    const t2 a = __builtin_convertvector((f32x2{keep_f32((float)y[0]), keep_f32((float)y[1])}), t2);
+    const t2 b = __builtin_convertvector((f32x2{keep_f32((float)y[2]), keep_f32((float)y[3])}), t2);
+    *reinterpret_cast<typename Vec<T, 4>::v *>(p) = typename Vec<T, 4>::v{a[0], a[1], b[0], b[1]};
+}
 
 // Where a lane's two pieces of four channels begin: piece b holds the partners of piece a where the pairs are rot / 2 apart.
 struct Pieces { int a, b; };
@@ -120,7 +129,6 @@ __device__ __forceinline__ uint8_t *block_of(const Kv4Cache &c, int32_t slot, in
 }
 
 // Eight channels (the ch-th eight) of a token's key or value for one head; four neighbouring lanes hold a group.  b == nullptr: nothing is stored.
-template <typename T, int N> struct Vec { typedef T v __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
 template <typename T> __device__ __forceinline__ void hold_key(uint8_t *b, int dim, int off, int ch, typename Vec<T, 8>::v r) {
     float x[8];
     uint32_t top = 0;
@@ -251,8 +259,8 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kern
         }
         T *out = is_q ? (T *)r.q_out + (row0 + row) * r.q_out_stride + h * r.dim
                : WRITE ? keys + ((size_t)row * r.n_kv + h - n_q) * r.dim : (T *)r.k_out + (row0 + row) * r.k_out_stride + (h - n_q) * r.dim;
-        *reinterpret_cast<v4 *>(out + p.a) = v4{round_to<T>(y[0]), round_to<T>(y[1]), round_to<T>(y[2]), round_to<T>(y[3])};
-        *reinterpret_cast<v4 *>(out + p.b) = v4{round_to<T>(y[4]), round_to<T>(y[5]), round_to<T>(y[6]), round_to<T>(y[7])};
+        store4<T>(out + p.a, y);
+        store4<T>(out + p.b, y + 4);
     }
     if constexpr (WRITE) {
         constexpr int AHEAD = 4;                            // values requested before the first is needed
