@@ -46,15 +46,15 @@ template <typename T, int N> __device__ __forceinline__ void split(float x, type
     }
 }
 
-// over the four lanes of a row (16 lanes apart)
-__device__ __forceinline__ float row_max(float v) {
-    v = fmaxf(v, __shfl_xor(v, 16, 64));
-    return fmaxf(v, __shfl_xor(v, 32, 64));
+// Over the four lanes of a row (16 lanes apart): a swap of a register with itself leaves, in its two results, what the lanes of a pair hold.
+template <typename F> __device__ __forceinline__ float over_row(float v, F f) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
 }
-__device__ __forceinline__ float row_sum(float v) {
-    v += __shfl_xor(v, 16, 64);
-    return v + __shfl_xor(v, 32, 64);
-}
+__device__ __forceinline__ float row_max(float v) { return over_row(v, [](float x, float y) { return fmaxf(x, y); }); }
+__device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float x, float y) { return x + y; }); }
 
 struct Seq { int row0, n, len; };      // first row, rows and keys of a sequence, within what the call allows
 __device__ __forceinline__ Seq sequence(const Kv4Attn &a, int b) {
@@ -77,16 +77,17 @@ __device__ __forceinline__ void seen(const Kv4Attn &a, const Seq &s, int i, int 
 }
 
 // ------------------------------------------------------------------------------------------------
-// Up to 16 rows (new tokens times query heads of one key head) a workgroup, the pages of its piece of the sequence dealt to four
-// waves.  S^T = K Q^T, 16 tokens an instruction: a lane holds row lane % 16 and, of a subtile, tokens 4 (lane / 16) + 0..3, which is
+// 16 NT rows (new tokens times query heads of one key head) a workgroup, the pages of its piece of the sequence dealt to four
+// waves, each with its own maximum and sums, which are joined at the end.  S^T = K Q^T, 16 tokens an instruction: a lane holds row lane % 16 and, of a subtile, tokens 4 (lane / 16) + 0..3, which is
 // the right operand of O^T = V^T P^T as it stands, two subtiles to an instruction.
 constexpr int kRows = 16;
+constexpr float kLag = 8.f;                       // base 2
 
 struct Tile { int first_lo, last_lo, first_hi, last_hi; };      // what the tile's first and last row see
 __device__ __forceinline__ Tile tile_range(const Kv4Attn &a, const Seq &s, int r0, int n_r, int G) {
     Tile t;
     seen(a, s, r0 / G, t.first_lo, t.last_lo);
-    seen(a, s, (min(r0 + kRows, n_r) - 1) / G, t.first_hi, t.last_hi);
+    seen(a, s, (min(r0 + a.tile, n_r) - 1) / G, t.first_hi, t.last_hi);
     return t;
 }
 
@@ -135,8 +136,8 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void unroll(F
     }
 }
 
-template <typename T, int NG>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 || NG > 4 ? 2 : 3) void kv4_attention_kernel(Kv4Attn a, int n_tiles) {
+template <typename T, int NG, int NT>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 || NG > 4 || NT * NG > 4 ? 2 : 3) void kv4_attention_kernel(Kv4Attn a, int n_tiles) {
     typedef typename Op<T>::t HT;
     typedef typename Half16<HT>::v8 v8;
     typedef T qv8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
@@ -146,19 +147,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
     __shared__ float ms[4][kRows], ls[4][kRows];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
     const int G = a.n_heads / a.cache.n_heads;
-    const int part = blockIdx.x % a.n_splits, tile = blockIdx.x / a.n_splits % n_tiles, pair = blockIdx.x / a.n_splits / n_tiles;
+    // pieces further back come last: only long sequences have them
+    const int n_pairs = a.n_seqs * a.cache.n_heads, tile = blockIdx.x % n_tiles, pair = blockIdx.x / n_tiles % n_pairs, part = blockIdx.x / n_tiles / n_pairs;
     const int b = pair / a.cache.n_heads, h = pair % a.cache.n_heads;
     const Seq sq = sequence(a, b);
-    const int n_r = sq.n * G, r0 = tile * kRows;
+    const int n_r = sq.n * G, r0 = tile * (kRows * NT);
     if (r0 >= n_r) return;
     const Tile tr = tile_range(a, sq, r0, n_r, G);
     const int lo = tr.first_lo, hi = tr.last_hi;
     const int p0 = max(lo / kKv4Page, part * a.split_pages);
     const int p1 = min(hi < lo ? 0 : hi / kKv4Page + 1, (part + 1) * a.split_pages);
     if (p0 >= p1 && a.n_splits > 1) return;
-    const int row = min(r0 + r, n_r - 1);
-    int first, last;
-    seen(a, sq, row / G, first, last);
+    int first[NT], last[NT];                      // what row r0 + 16 n + r sees
+#pragma unroll
+    for (int n = 0; n < NT; ++n) seen(a, sq, min(r0 + kRows * n + r, n_r - 1) / G, first[n], last[n]);
 
     // The wave's pages (every fourth of the piece): first those that every row sees whole, f0 .. f1 - 1, then the ones after and before.
     const int f0 = min(max((tr.first_hi + kKv4Page - 1) / kKv4Page, p0), p1), f1 = max(min((tr.last_lo + 1) / kKv4Page, p1), f0);
@@ -174,16 +176,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
     const size_t page_bytes = (size_t)a.cache.n_heads * kv4_block_bytes(DIM);
     auto entry = [&](int i) { return i < n_pages ? table[page_at(i)] : -1; };
     auto valid = [&](int id) { return id >= 0 && id < a.cache.n_pages; };
-    auto block = [&](int id) { return base + (size_t)id * page_bytes; };
+    // what comes next is requested always, from some page where there is none: the compiler counts the loads on their way
+    auto block = [&](int id) { return base + (size_t)(valid(id) ? id : 0) * page_bytes; };
     int id = entry(0), id_next = entry(1);
     Page<NG> pg;
-    if (valid(id)) {
-        load_keys<NG>(pg, block(id), r, j);
-        load_values<NG>(pg, block(id), r, j);
-    }
+    load_keys<NG>(pg, block(id), r, j);
+    load_values<NG>(pg, block(id), r, j);
 
-    v8 qf[NG][NP];
-    {
+    v8 qf[NT][NG][NP];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int row = min(r0 + kRows * n + r, n_r - 1);
         const T *q = (const T *)a.q + (int64_t)(sq.row0 + row / G) * a.q_stride + (int64_t)(h * G + row % G) * DIM;
 #pragma unroll
         for (int s = 0; s < NG; ++s) {
@@ -194,23 +197,29 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
                 if constexpr (NP == 1) p[0] = x[e];
                 else split<T, NP>(x[e], p);
 #pragma unroll
-                for (int c = 0; c < NP; ++c) qf[s][c][e] = p[c];
+                for (int c = 0; c < NP; ++c) qf[n][s][c][e] = p[c];
             }
         }
     }
-    f32x4v o[NG][2];
+    f32x4v o[NT][NG][2];
+    float m[NT], l[NT];                           // of the row (m scaled, base 2); of the lane's tokens of the row
 #pragma unroll
-    for (int g = 0; g < NG; ++g) o[g][0] = o[g][1] = f32x4v{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;                 // of the row (m scaled, base 2); of the lane's tokens of the row
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) o[n][g][0] = o[n][g][1] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        m[n] = -INFINITY;
+        l[n] = 0.f;
+    }
 
     // One page: scores, then the keys of the next page are requested; softmax; values, then those of the next page.
     auto step = [&](auto masked_, int page) {
         constexpr bool MASKED = decltype(masked_)::value;
         const int t0 = page * kKv4Page;
-        const bool more = valid(id_next);
-        f32x4v sc[4];
+        f32x4v sc[NT][4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sc[t] = f32x4v{0.f, 0.f, 0.f, 0.f};
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sc[n][t] = f32x4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int t = 0; t < 4; t += 2)
 #pragma unroll
@@ -220,32 +229,41 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
                     v8 kf;
                     decode8<HT>(pg.k[u][s], pow2_byte(pg.ks[s / 4], u), kf);
 #pragma unroll
-                    for (int c = 0; c < NP; ++c) sc[u] = Mfma16<HT>::run(kf, qf[s][c], sc[u]);
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int c = 0; c < NP; ++c) sc[n][u] = Mfma16<HT>::run(kf, qf[n][s][c], sc[n][u]);
                 }
                 __builtin_amdgcn_sched_barrier(0);      // or all conversions of the page are begun at once, in as many registers
             }
-        if (more) load_keys<NG>(pg, block(id_next), r, j);
-        float mx = -INFINITY;
+        load_keys<NG>(pg, block(id_next), r, j);
+        float m_use[NT];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int n = 0; n < NT; ++n) {
+            float mx = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int key = t0 + 16 * t + 4 * j + e;
-                if (MASKED) sc[t][e] = key >= first && key <= last ? sc[t][e] : -INFINITY;
-                mx = fmaxf(mx, sc[t][e]);
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int key = t0 + 16 * t + 4 * j + e;
+                    if (MASKED) sc[n][t][e] = key >= first[n] && key <= last[n] ? sc[n][t][e] : -INFINITY;
+                    mx = fmaxf(mx, sc[n][t][e]);
+                }
+            // The running maximum is only a reference: it moves when a score of some row is more than 2^kLag times over it, so that pages seldom
+            // exchange anything between lanes or touch the sums.  Probabilities then reach 2^kLag, which every operand type holds as exactly as 1.
+            mx *= a.scale_log2;
+            if (__builtin_amdgcn_ballot_w64(!(mx <= m[n] + kLag)) != 0) {
+                const float m_new = fmaxf(m[n], row_max(mx));
+                const float corr = __builtin_amdgcn_exp2f(m[n] - (m_new == -INFINITY ? 0.f : m_new));
+                l[n] *= corr;
+#pragma unroll
+                for (int g = 0; g < NG; ++g)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[n][g][c][e] *= corr;
+                m[n] = m_new;
             }
-        const float m_new = fmaxf(m, row_max(mx) * a.scale_log2);
-        const float m_use = m_new == -INFINITY ? 0.f : m_new;
-        if (__builtin_amdgcn_ballot_w64(m_new != m) != 0) {
-            const float corr = __builtin_amdgcn_exp2f(m - m_use);
-            l *= corr;
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[g][c][e] *= corr;
-            m = m_new;
+            m_use[n] = m[n] == -INFINITY ? 0.f : m[n];
         }
         // value scales as floats, byte k of a dword in vf[i][k], still dealt over the lanes
         u32 sf[Page<NG>::VS][4];
@@ -272,17 +290,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
         }
         unroll<2>([&](auto half_) {
             constexpr int t = 2 * decltype(half_)::value;
-            v8 pf[NP];
+            v8 pf[NT][NP];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(sc[t + e / 4][e % 4], a.scale_log2, -m_use));
-                HT p[NP];
-                if constexpr (NP == 1) p[0] = from_f32<HT>(x);
-                else { split<T, NP>(x, p); l += x; }
+            for (int n = 0; n < NT; ++n) {
 #pragma unroll
-                for (int c = 0; c < NP; ++c) pf[c][e] = p[c];
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(sc[n][t + e / 4][e % 4], a.scale_log2, -m_use[n]));
+                    HT p[NP];
+                    if constexpr (NP == 1) p[0] = from_f32<HT>(x);
+                    else { split<T, NP>(x, p); l[n] += x; }
+#pragma unroll
+                    for (int c = 0; c < NP; ++c) pf[n][c][e] = p[c];
+                }
+                if constexpr (NP == 1) l[n] = Half16<HT>::add_all(pf[n][0], l[n]);
             }
-            if constexpr (NP == 1) l = Half16<HT>::add_all(pf[0], l);
             unroll<NG>([&](auto g_) {
                 constexpr int g = decltype(g_)::value;
                 v8 vf[2];
@@ -297,21 +318,25 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
                     vf[1][e] = x1;
                 });
 #pragma unroll
-                for (int c = 0; c < NP; ++c) {
-                    o[g][0] = Mfma16<HT>::run(vf[0], pf[c], o[g][0]);
-                    o[g][1] = Mfma16<HT>::run(vf[1], pf[c], o[g][1]);
-                }
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int c = 0; c < NP; ++c) {
+                        o[n][g][0] = Mfma16<HT>::run(vf[0], pf[n][c], o[n][g][0]);
+                        o[n][g][1] = Mfma16<HT>::run(vf[1], pf[n][c], o[n][g][1]);
+                    }
                 __builtin_amdgcn_sched_barrier(0);
             });
         });
-        if (more) load_values<NG>(pg, block(id_next), r, j);
+        load_values<NG>(pg, block(id_next), r, j);
         if (MASKED && __builtin_amdgcn_ballot_w64(nan_hidden) != 0) {
             const uint8_t *blk = block(id);
             for (int off = 0; off < kKv4Page; ++off)
 #pragma unroll
                 for (int g = 0; g < NG; ++g)
-                    if (t0 + off >= first && t0 + off <= last && blk[kv4_v_scale(DIM, off) + g] == 255)
-                        o[g][0] = o[g][1] = f32x4v{NAN, NAN, NAN, NAN};
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        if (t0 + off >= first[n] && t0 + off <= last[n] && blk[kv4_v_scale(DIM, off) + g] == 255)
+                            o[n][g][0] = o[n][g][1] = f32x4v{NAN, NAN, NAN, NAN};
         }
     };
     auto walk = [&](auto masked_, int from, int to) {
@@ -319,7 +344,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
             const int id_after = entry(i + 2);
             if (valid(id)) {
                 step(masked_, page_at(i));
-            } else if (valid(id_next)) {          // this one is not seen, and the next not on its way yet
+            } else {                              // not seen, and the next page not on its way yet
                 load_keys<NG>(pg, block(id_next), r, j);
                 load_values<NG>(pg, block(id_next), r, j);
             }
@@ -329,112 +354,128 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
     };
     walk(std::false_type{}, 0, n_whole);
     walk(std::true_type{}, n_whole, n_pages);
-    l = row_sum(l);
-    if (j == 0) { ms[wave][r] = m; ls[wave][r] = l; }
 
-    // the four waves' sums, RG groups at a time
+    // the four waves' sums, 16 rows and RG groups at a time
     const int orow = threadIdx.x >> 4, oc = threadIdx.x & 15;      // 16 threads a row, RDIM / 16 channels each
     constexpr int PER = RDIM / 16;
-    const bool live = r0 + orow < n_r;
-    const int64_t at = sq.row0 + (r0 + orow) / G;
-    const int head = h * G + (r0 + orow) % G;
 #pragma unroll
-    for (int g0 = 0; g0 < NG; g0 += RG) {
-        if (g0) __syncthreads();
+    for (int n = 0; n < NT; ++n) {
+        const int rn = r0 + kRows * n;
+        if (rn >= n_r) break;
+        if (n) __syncthreads();
+        const float ln = row_sum(l[n]);
+        if (j == 0) { ms[wave][r] = m[n]; ls[wave][r] = ln; }
+        const bool live = rn + orow < n_r;
+        const int64_t at = sq.row0 + (rn + orow) / G;
+        const int head = h * G + (rn + orow) % G;
 #pragma unroll
-        for (int g = 0; g < RG; ++g) {
-            float *d = &acc[wave][r * LD + 32 * g + 8 * j];
-            const f32x4v x = o[g0 + g][0], y = o[g0 + g][1];
-            *reinterpret_cast<f32x4 *>(d) = f32x4{x[0], y[0], x[1], y[1]};
-            *reinterpret_cast<f32x4 *>(d + 4) = f32x4{x[2], y[2], x[3], y[3]};
-        }
-        __syncthreads();
-        const float mj = fmaxf(fmaxf(ms[0][orow], ms[1][orow]), fmaxf(ms[2][orow], ms[3][orow]));
-        const float mu = mj == -INFINITY ? 0.f : mj;
-        float w[4], den = 0.f, sum[PER];
+        for (int g0 = 0; g0 < NG; g0 += RG) {
+            if (g0) __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { w[i] = __builtin_amdgcn_exp2f(ms[i][orow] - mu); den = fmaf(w[i], ls[i][orow], den); }
+            for (int g = 0; g < RG; ++g) {
+                float *d = &acc[wave][r * LD + 32 * g + 8 * j];
+                const f32x4v x = o[n][g0 + g][0], y = o[n][g0 + g][1];
+                *reinterpret_cast<f32x4 *>(d) = f32x4{x[0], y[0], x[1], y[1]};
+                *reinterpret_cast<f32x4 *>(d + 4) = f32x4{x[2], y[2], x[3], y[3]};
+            }
+            __syncthreads();
+            const float mj = fmaxf(fmaxf(ms[0][orow], ms[1][orow]), fmaxf(ms[2][orow], ms[3][orow]));
+            const float mu = mj == -INFINITY ? 0.f : mj;
+            float w[4], den = 0.f, sum[PER];
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            sum[e] = 0.f;
+            for (int i = 0; i < 4; ++i) { w[i] = __builtin_amdgcn_exp2f(ms[i][orow] - mu); den = fmaf(w[i], ls[i][orow], den); }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[e] = fmaf(w[i], acc[i][orow * LD + oc * PER + e], sum[e]);
-        }
-        if (!live) continue;
-        if (a.n_splits == 1) {
-            T *out = (T *)a.o + at * a.o_stride + (int64_t)head * DIM + 32 * g0 + oc * PER;
-            const float inv = den == 0.f ? 0.f : 1.f / den;
+            for (int e = 0; e < PER; ++e) {
+                sum[e] = 0.f;
 #pragma unroll
-            for (int e = 0; e < PER; ++e) out[e] = from_f32<T>(den == 0.f ? 0.f : sum[e] * inv);
-        } else {
-            float *out = a.partial + ((at * a.n_heads + head) * a.n_splits + part) * (DIM + 2);
+                for (int i = 0; i < 4; ++i) sum[e] = fmaf(w[i], acc[i][orow * LD + oc * PER + e], sum[e]);
+            }
+            if (!live) continue;
+            if (a.n_splits == 1) {
+                T *out = (T *)a.o + at * a.o_stride + (int64_t)head * DIM + 32 * g0 + oc * PER;
+                const float inv = den == 0.f ? 0.f : 1.f / den;
 #pragma unroll
-            for (int e = 0; e < PER; ++e) out[32 * g0 + oc * PER + e] = sum[e];
-            if (g0 == 0 && oc == 0) { out[DIM] = mj; out[DIM + 1] = den; }
-        }
-    }
-}
-
-// Joins the pieces of one row and head: a wave each, in the order of the pieces.
-template <typename T>
-__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
-    const int G = a.n_heads / a.cache.n_heads, dim = a.cache.dim, lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int i = (int)(id % a.max_q);
-    const int head = (int)(id / a.max_q % a.n_heads);
-    const int64_t b = id / a.max_q / a.n_heads;
-    if (b >= a.n_seqs) return;
-    const Seq sq = sequence(a, (int)b);
-    if (i >= sq.n) return;
-    const Tile tr = tile_range(a, sq, (i * G + head % G) / kRows * kRows, sq.n * G, G);
-    const int lo = tr.first_lo, hi = tr.last_hi;
-    const int s0 = lo / kKv4Page / a.split_pages, s1 = hi < lo ? s0 : hi / kKv4Page / a.split_pages + 1;
-    const int64_t at = sq.row0 + i;
-    const float *p = a.partial + (at * a.n_heads + head) * a.n_splits * (dim + 2);
-    float m = -INFINITY;
-    for (int s = s0 + lane; s < s1; s += 64) m = fmaxf(m, p[(int64_t)s * (dim + 2) + dim]);
-    m = wave_max(m);
-    const float mu = m == -INFINITY ? 0.f : m;
-    float den = 0.f, sum[4] = {};
-    for (int c0 = s0; c0 < s1; c0 += 64) {            // a lane a piece: its weight
-        const int n = min(64, s1 - c0);
-        const float *pc = p + (int64_t)c0 * (dim + 2);
-        float w = 0.f;
-        if (lane < n) {
-            w = __builtin_amdgcn_exp2f(pc[(int64_t)lane * (dim + 2) + dim] - mu);
-            den = fmaf(w, pc[(int64_t)lane * (dim + 2) + dim + 1], den);
-        }
-        for (int s = 0; s < n; s += 8) {              // eight pieces requested at a time
-            float x[8][4];
+                for (int e = 0; e < PER; ++e) out[e] = from_f32<T>(den == 0.f ? 0.f : sum[e] * inv);
+            } else {
+                const int64_t piece = (at * a.n_heads + head) * a.n_splits + part;
+                float *out = a.partial + piece * DIM + 32 * g0 + oc * PER;
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    x[u][c] = s + u < n && lane + 64 * c < dim ? pc[(int64_t)(s + u) * (dim + 2) + lane + 64 * c] : 0.f;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const float wu = __shfl(w, (s + u) & 63, 64);
-                if (s + u < n)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) sum[c] = fmaf(wu, x[u][c], sum[c]);
+                for (int e = 0; e < PER; ++e) out[e] = sum[e];
+                if (g0 == 0 && oc == 0) { a.partial_ml[2 * piece] = mj; a.partial_ml[2 * piece + 1] = den; }
             }
         }
     }
-    den = wave_sum(den);
-    T *out = (T *)a.o + at * a.o_stride + (int64_t)head * dim;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (lane + 64 * c < dim) out[lane + 64 * c] = from_f32<T>(den == 0.f ? 0.f : sum[c] / den);
 }
 
-int row_tiles(const Kv4Attn &a) { return (int)(((int64_t)a.max_q * (a.n_heads / a.cache.n_heads) + kRows - 1) / kRows); }
+// Joins the pieces of a row and head: 16 lanes, or four times 16 (WIDE) that take every fourth piece.
+template <typename T, int NG, bool WIDE>
+__global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
+    constexpr int DIM = 32 * NG, PER = 2 * NG, AHEAD = NG > 4 ? 4 : 8, LANES = WIDE ? 64 : 16, WAYS = LANES / 16;
+    typedef T tv __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
+    typedef float fv __attribute__((ext_vector_type(PER), aligned(8)));
+    const int G = a.n_heads / a.cache.n_heads, c = threadIdx.x & 15, way = (threadIdx.x & (LANES - 1)) >> 4;
+    const int64_t id = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int head = (int)(id % a.n_heads), i = (int)(id / a.n_heads % a.max_q);
+    const int64_t b = id / a.n_heads / a.max_q;
+    if (b >= a.n_seqs) return;
+    const Seq sq = sequence(a, (int)b);
+    if (i >= sq.n) return;
+    const Tile tr = tile_range(a, sq, (i * G + head % G) / a.tile * a.tile, sq.n * G, G);
+    const int lo = tr.first_lo, hi = tr.last_hi;
+    const int s0 = lo / kKv4Page / a.split_pages, s1 = hi < lo ? s0 : hi / kKv4Page / a.split_pages + 1;      // the pieces that have been written
+    const int64_t at = sq.row0 + i, piece0 = (at * a.n_heads + head) * a.n_splits;
+    const float *ml = a.partial_ml + 2 * piece0, *p = a.partial + piece0 * DIM + c * PER;
+    float m = -INFINITY;
+    for (int s = s0 + (threadIdx.x & (LANES - 1)); s < s1; s += LANES) m = fmaxf(m, ml[2 * s]);
+#pragma unroll
+    for (int o = LANES / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, LANES));
+    const float mu = m == -INFINITY ? 0.f : m;
+    float den = 0.f, sum[PER] = {};
+    for (int s = s0 + way; s < s1; s += WAYS * AHEAD) {
+        fv x[AHEAD];
+        float w[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int su = s + u * WAYS, at_u = min(su, s1 - 1);
+            x[u] = *reinterpret_cast<const fv *>(p + (int64_t)at_u * DIM);
+            w[u] = __builtin_amdgcn_exp2f(ml[2 * at_u] - mu);
+            if (su < s1) den = fmaf(w[u], ml[2 * at_u + 1], den);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (s + u * WAYS < s1)
+#pragma unroll
+                for (int e = 0; e < PER; ++e) sum[e] = fmaf(w[u], x[u][e], sum[e]);
+    }
+    if constexpr (WIDE) {
+        den = row_sum(den);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) sum[e] = row_sum(sum[e]);
+        if (way) return;
+    }
+    const float inv = den == 0.f ? 0.f : 1.f / den;
+    tv out;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) out[e] = from_f32<T>(den == 0.f ? 0.f : sum[e] * inv);
+    *reinterpret_cast<tv *>((T *)a.o + at * a.o_stride + (int64_t)head * DIM + c * PER) = out;
+}
+
+int row_tiles(const Kv4Attn &a) { return (int)(((int64_t)a.max_q * (a.n_heads / a.cache.n_heads) + a.tile - 1) / a.tile); }
 
 }  // namespace
 
-void kv4_attention_split(Kv4Attn &a) {
+void kv4_attention_plan(Kv4Attn &a, bool is_f32) {
+    const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.cache.n_heads);
     const int pages = (a.max_kv + kKv4Page - 1) / kKv4Page;
-    const int64_t have = (int64_t)a.n_seqs * a.cache.n_heads * row_tiles(a);
-    int64_t want = have ? (2048 + have - 1) / have : 1;
+    // 32 rows a workgroup share the conversions of a page (8 sequences of 4000 keys, 8 key heads of 64, 1200 rows each: 156 us with 16 rows, 129
+    // with 32), but a short launch is over sooner on 16 (one sequence of 1000 keys, 24 rows: 9.0 us, 10.4 with 32).  Registers hold two
+    // such tiles up to heads of 128.
+    const int64_t n_pairs = (int64_t)a.n_seqs * a.cache.n_heads;
+    a.tile = rows > kRows && !is_f32 && a.cache.dim <= 128 && n_pairs * pages >= 256 ? 2 * kRows : kRows;
+    // Pieces: workgroups for the chip a few times over (16 sequences of 20000 to 65536 keys, 8 key heads of 128: 1024 workgroups 171 us, 2048 148,
+    // 4096 152 and a longer join); fewer of 32 rows, whose sums take longer to write and join than a few pages to read.
+    const int64_t have = n_pairs * row_tiles(a), aim = a.tile == kRows ? 2048 : 1024;
+    int64_t want = have ? (aim + have - 1) / have : 1;
     want = want < 1 ? 1 : want;
     int per = (int)((pages + want - 1) / want);
     per = (per + 3) / 4 * 4;                      // a page for each wave
@@ -443,7 +484,9 @@ void kv4_attention_split(Kv4Attn &a) {
     if (a.n_splits < 1) a.n_splits = 1;
 }
 
-int64_t kv4_attention_grid(const Kv4Attn &a) { return (int64_t)a.n_seqs * a.cache.n_heads * row_tiles(a) * a.n_splits; }
+int64_t kv4_attention_grid(const Kv4Attn &a) {
+    return (int64_t)a.n_seqs * a.cache.n_heads * row_tiles(a) * a.n_splits;
+}
 
 size_t kv4_attention_workspace(const Kv4Attn &a) {
     return a.n_splits > 1 ? (size_t)a.n_rows * a.n_heads * a.n_splits * (a.cache.dim + 2) * sizeof(float) : 0;
@@ -454,15 +497,41 @@ template <typename T> void launch_kv4_attention(const Kv4Attn &a, hipStream_t s)
     const int64_t n = kv4_attention_grid(a);
     if (n <= 0 || a.n_rows <= 0) return;
     const dim3 grid((unsigned)n), block(256);
-    switch (a.cache.dim / 32) {
-        case 1: hipLaunchKernelGGL((kv4_attention_kernel<T, 1>), grid, block, 0, s, a, n_tiles); break;
-        case 2: hipLaunchKernelGGL((kv4_attention_kernel<T, 2>), grid, block, 0, s, a, n_tiles); break;
-        case 4: hipLaunchKernelGGL((kv4_attention_kernel<T, 4>), grid, block, 0, s, a, n_tiles); break;
-        default: hipLaunchKernelGGL((kv4_attention_kernel<T, 8>), grid, block, 0, s, a, n_tiles); break;
+    const int nt = a.tile / kRows;
+#define SJD_KV4_ATTEND(NG, NT) hipLaunchKernelGGL((kv4_attention_kernel<T, NG, NT>), grid, block, 0, s, a, n_tiles)
+    if constexpr (sizeof(T) == 4) {
+        switch (a.cache.dim / 32) {
+            case 1: SJD_KV4_ATTEND(1, 1); break;
+            case 2: SJD_KV4_ATTEND(2, 1); break;
+            case 4: SJD_KV4_ATTEND(4, 1); break;
+            default: SJD_KV4_ATTEND(8, 1); break;
+        }
+    } else {
+        switch (a.cache.dim / 32 * 8 + nt) {
+            case 8 + 1: SJD_KV4_ATTEND(1, 1); break;
+            case 8 + 2: SJD_KV4_ATTEND(1, 2); break;
+            case 16 + 1: SJD_KV4_ATTEND(2, 1); break;
+            case 16 + 2: SJD_KV4_ATTEND(2, 2); break;
+            case 32 + 1: SJD_KV4_ATTEND(4, 1); break;
+            case 32 + 2: SJD_KV4_ATTEND(4, 2); break;
+            default: SJD_KV4_ATTEND(8, 1); break;
+        }
     }
+#undef SJD_KV4_ATTEND
     if (a.n_splits > 1) {
         const int64_t rows = (int64_t)a.n_seqs * a.n_heads * a.max_q;
-        hipLaunchKernelGGL((kv4_join_kernel<T>), dim3((unsigned)((rows + 3) / 4)), block, 0, s, a);
+        const bool wide = a.n_splits > 8;         // one round of requests for 16 lanes
+        const dim3 joins((unsigned)((rows + (wide ? 3 : 15)) / (wide ? 4 : 16)));
+#define SJD_KV4_JOIN(NG)                                                                       \
+    if (wide) hipLaunchKernelGGL((kv4_join_kernel<T, NG, true>), joins, block, 0, s, a);      \
+    else hipLaunchKernelGGL((kv4_join_kernel<T, NG, false>), joins, block, 0, s, a)
+        switch (a.cache.dim / 32) {
+            case 1: SJD_KV4_JOIN(1); break;
+            case 2: SJD_KV4_JOIN(2); break;
+            case 4: SJD_KV4_JOIN(4); break;
+            default: SJD_KV4_JOIN(8); break;
+        }
+#undef SJD_KV4_JOIN
     }
 }
 template void launch_kv4_attention<float>(const Kv4Attn &, hipStream_t);

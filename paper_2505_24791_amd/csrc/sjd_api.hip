@@ -1582,7 +1582,7 @@ int check_attention(const sjd_kv4 *c, const sjd_kv4_attention *g, Kv4Attn *out) 
     a.max_kv = (int)((int64_t)g->max_pages * SJD_KV4_PAGE < g->max_kv ? (int64_t)g->max_pages * SJD_KV4_PAGE : g->max_kv);
     a.causal = g->causal != 0; a.skip = g->skip_nearest; a.window = g->window;
     a.scale_log2 = g->scale * 1.44269504088896340736f;
-    kv4_attention_split(a);
+    kv4_attention_plan(a, c->dtype == SJD_DTYPE_F32);
     if (kv4_attention_grid(a) > INT32_MAX) return fail(SJD_EINVAL, "too many rows and sequences for one call");
     *out = a;
     return SJD_OK;
@@ -1692,6 +1692,7 @@ int sjd_op_kv4_attention(const sjd_kv4 *cache, const sjd_kv4_attention *args, vo
     if (need && (!args->workspace_dev || args->workspace_bytes < need || (uintptr_t)args->workspace_dev % 16))
         return fail(SJD_EINVAL, "this call needs %zu bytes of workspace on a 16-byte boundary", need);
     a.partial = (float *)args->workspace_dev;
+    a.partial_ml = a.partial + (size_t)a.n_rows * a.n_heads * a.n_splits * a.cache.dim;
     hipStream_t s = (hipStream_t)hip_stream;
     if (cache->dtype == SJD_DTYPE_F32) launch_kv4_attention<float>(a, s);
     else if (cache->dtype == SJD_DTYPE_BF16) launch_kv4_attention<bf16>(a, s);

@@ -281,6 +281,10 @@ ATTEND = [
     (1, 2, 128, [77, 640], [9, 2], False, 0, 0),
     (2, 4, 64, [333, 5], [4, 5], False, 2, 100),
     (1, 8, 64, [2, 700], [2, 40], True, 5, 0),
+    (2, 8, 128, [500, 70, 65], [60, 70, 1], True, 0, 0),
+    (1, 4, 128, [300], [100], True, 2, 33),
+    (1, 1, 32, [200, 1000], [200, 129], True, 0, 0),
+    (1, 3, 128, [190, 64], [50, 64], False, 1, 0),
 ]
 
 
