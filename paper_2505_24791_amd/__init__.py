@@ -216,61 +216,64 @@ def op_attention_h16(qkv, n_samples, T, H):
 
 KV4_PAGE = 64          # tokens of a page of the 4-bit cache
 _NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
-_ROW_DTYPES = None     # torch types of rows -> DTYPE_* (torch is imported on first use)
+_rt = None             # what the calls below use of the library and of torch, once both are loaded
 
 
-def _row_dtype(torch_dtype) -> int:
-    global _ROW_DTYPES
-    if _ROW_DTYPES is None:
-        import torch
-        _ROW_DTYPES = {torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
-    code = _ROW_DTYPES.get(torch_dtype)
-    if code is None:
-        _refuse(f"rows must be float16, bfloat16 or float32, not {torch_dtype}")
-    return code
+def _runtime():
+    global _rt
+    import torch
+    dtypes = {torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16, torch.float32: DTYPE_F32}
+    # torch.cuda.current_stream() makes two objects around this number: 2.6 us of a call that takes 8
+    _rt = (load_library(), torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, torch.cuda.device, torch.int32, dtypes)
+    return _rt
 
 
 def _refuse(what: str):
     raise SjdError(SJD_EINVAL, what)
 
 
-# The checks of the calls below run for every token of a serving loop: messages are made only where one fails.
+def _row_dtype(torch_dtype) -> int:
+    code = (_rt or _runtime())[5].get(torch_dtype)
+    if code is None:
+        _refuse(f"rows must be float16, bfloat16 or float32, not {torch_dtype}")
+    return code
+
+
+# The checks of the calls below run for every token of a serving loop: messages are made only where one fails, and a tensor that a call
+# made itself is not looked at again.
 def _rows3(t, what: str, dtype, device: int):
-    """The shape of t [rows, heads, head_dim] (any row stride, the heads of a row following one another)."""
-    if t.dtype is not dtype or not t.is_cuda or t.get_device() != device or t.dim() != 3:
+    """Shape and row stride of t [rows, heads, head_dim], the heads of a row following one another."""
+    shape, stride = t.shape, t.stride()
+    if t.dtype is not dtype or t.get_device() != device or len(shape) != 3:
         _refuse(f"{what}: need a {dtype} tensor [rows, heads, head_dim] on cuda:{device}")
-    shape = t.shape
-    n, h, d = shape
-    if n and not ((d == 1 or t.stride(2) == 1) and (h == 1 or t.stride(1) == d)):
+    if ((stride[1] != shape[2] and shape[1] != 1) or (stride[2] != 1 and shape[2] != 1)) and shape[0]:
         _refuse(f"{what}: the heads of a row must follow one another")
-    return shape
+    return shape, stride[0]
+
+
+def _into(out, like, shape, dtype, what: str, device: int):
+    """(out, its row stride): a new tensor, or the one that the caller gave, checked."""
+    if out is None:
+        return like.new_empty(shape, dtype=dtype), shape[1] * shape[2]
+    got, stride = _rows3(out, what, dtype, device)
+    if got != shape:
+        _refuse(f"{what}: need the shape {tuple(shape)}")
+    return out, stride
 
 
 def _ints(t, what: str, shape, device: int) -> int:
-    if t.dtype is not _int32() or not t.is_cuda or t.get_device() != device or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not _rt[4] or t.get_device() != device or t.shape != shape or not t.is_contiguous():
         _refuse(f"{what}: need a contiguous int32 tensor {tuple(shape)} on cuda:{device}")
     return t.data_ptr()
 
 
-_I32 = None
-
-
-def _int32():
-    global _I32
-    if _I32 is None:
-        import torch
-        _I32 = torch.int32
-    return _I32
-
-
 def _launch(device: int, fn, *args) -> None:
     """Calls fn(*args, stream) with the tensors' device current, on that device's current stream."""
-    import torch
-    stream = torch._C._cuda_getCurrentRawStream(device)     # torch.cuda.current_stream() makes two objects first: 2.6 us of a call
-    if device == torch.cuda.current_device():
+    stream = _rt[1](device)
+    if device == _rt[2]():
         rc = fn(*args, stream)
     else:
-        with torch.cuda.device(device):
+        with _rt[3](device):
             rc = fn(*args, stream)
     if rc:
         _check(rc)
@@ -325,26 +328,21 @@ def op_qk_norm_rope(q, k, pos, opts: QkOpts, *, q_out=None, k_out=None):
         _refuse("need q or k")
     dtype, device = some.dtype, some.get_device()
     code = _row_dtype(dtype)
-    n, _, dim = _rows3(some, "q or k", dtype, device)
     qp = qs = qh = qo = qos = kp = ks = kh = ko = kos = 0
     if q is not None:
-        shape = q.shape
-        if q_out is None:
-            q_out = q.new_empty(shape)
-        elif _rows3(q_out, "q_out", dtype, device) != shape:
-            _refuse("q_out: need the shape of q")
-        qp, qs, qh, qo, qos = q.data_ptr(), q.stride(0), shape[1], q_out.data_ptr(), q_out.stride(0)
+        shape, qs = _rows3(q, "q", dtype, device)
+        n, qh, dim = shape
+        q_out, qos = _into(q_out, q, shape, dtype, "q_out", device)
+        qp, qo = q.data_ptr(), q_out.data_ptr()
     if k is not None:
-        shape = _rows3(k, "k", dtype, device)
-        if shape[0] != n or shape[2] != dim:
+        shape, ks = _rows3(k, "k", dtype, device)
+        if q is not None and (shape[0] != n or shape[2] != dim):
             _refuse("k: other rows or another head size than q")
-        if k_out is None:
-            k_out = k.new_empty(shape)
-        elif _rows3(k_out, "k_out", dtype, device) != shape:
-            _refuse("k_out: need the shape of k")
-        kp, ks, kh, ko, kos = k.data_ptr(), k.stride(0), shape[1], k_out.data_ptr(), k_out.stride(0)
+        n, kh, dim = shape
+        k_out, kos = _into(k_out, k, shape, dtype, "k_out", device)
+        kp, ko = k.data_ptr(), k_out.data_ptr()
     p = _ints(pos, "pos", (n, opts.n_axes), device) if opts.n_axes else None
-    _launch(device, load_library().sjd_op_qk_norm_rope, code, opts._for(dim, device), p, qp, qs, qh, kp, ks, kh, dim, qo, qos, ko, kos, n)
+    _launch(device, _rt[0].sjd_op_qk_norm_rope, code, opts._for(dim, device), p, qp, qs, qh, kp, ks, kh, dim, qo, qos, ko, kos, n)
     return q_out, k_out
 
 
@@ -367,9 +365,10 @@ class Kv4Cache:
         return cls(torch.zeros((n_pages, kv_heads, 68 * head_dim), dtype=torch.uint8, device=device), dtype)
 
     def _kv(self, t, what: str, n: int):
-        if _rows3(t, what, self.dtype, self.device) != (n, self.kv_heads, self.head_dim):
+        shape, stride = _rows3(t, what, self.dtype, self.device)
+        if shape != (n, self.kv_heads, self.head_dim):
             _refuse(f"{what}: need [{n}, {self.kv_heads}, {self.head_dim}]")
-        return t.data_ptr(), t.stride(0)
+        return t.data_ptr(), stride
 
 
 def op_kv4_write(cache: Kv4Cache, k, v, slot, *, opts: Optional[QkOpts] = None, pos=None, q=None, q_out=None):
@@ -388,29 +387,23 @@ def op_kv4_write(cache: Kv4Cache, k, v, slot, *, opts: Optional[QkOpts] = None, 
     if q is not None:
         if opts is None:
             _refuse("queries need opts")
-        shape = _rows3(q, "q", cache.dtype, device)
+        shape, qs = _rows3(q, "q", cache.dtype, device)
         if shape[0] != n or shape[2] != dim:
             _refuse("q: other rows or another head size")
-        if q_out is None:
-            q_out = q.new_empty(shape)
-        elif _rows3(q_out, "q_out", cache.dtype, device) != shape:
-            _refuse("q_out: need the shape of q")
-        qp, qs, heads, qo, qos = q.data_ptr(), q.stride(0), shape[1], q_out.data_ptr(), q_out.stride(0)
-    _launch(device, load_library().sjd_op_kv4_write, cache.address, sp, kp, ks, vp_, vs, n, op, pp, qp, qs, heads, qo, qos)
+        q_out, qos = _into(q_out, q, shape, cache.dtype, "q_out", device)
+        qp, heads, qo = q.data_ptr(), shape[1], q_out.data_ptr()
+    _launch(device, _rt[0].sjd_op_kv4_write, cache.address, sp, kp, ks, vp_, vs, n, op, pp, qp, qs, heads, qo, qos)
     return q_out if q is not None else None
 
 
 def op_kv4_read(cache: Kv4Cache, slot, *, k_out=None, v_out=None):
     """``sjd_op_kv4_read``: the tokens ``slot`` [rows] int32 of the cache, (k, v) [rows, kv_heads, head_dim]; zeros for a slot outside it."""
-    n = slot.shape[0]
-    sp = _ints(slot, "slot", (n,), cache.device)
+    n, device = slot.shape[0], cache.device
+    sp = _ints(slot, "slot", (n,), device)
     shape = (n, cache.kv_heads, cache.head_dim)
-    if k_out is None:
-        k_out = cache.pages.new_empty(shape, dtype=cache.dtype)
-    if v_out is None:
-        v_out = cache.pages.new_empty(shape, dtype=cache.dtype)
-    (kp, ks), (vp_, vs) = cache._kv(k_out, "k_out", n), cache._kv(v_out, "v_out", n)
-    _launch(cache.device, load_library().sjd_op_kv4_read, cache.address, sp, kp, ks, vp_, vs, n)
+    k_out, ks = _into(k_out, cache.pages, shape, cache.dtype, "k_out", device)
+    v_out, vs = _into(v_out, cache.pages, shape, cache.dtype, "v_out", device)
+    _launch(device, _rt[0].sjd_op_kv4_read, cache.address, sp, k_out.data_ptr(), ks, v_out.data_ptr(), vs, n)
     return k_out, v_out
 
 
@@ -421,23 +414,21 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
     each).  max_q and max_kv bound the rows and keys of a sequence (max_kv None: all that the table has room for).  Rows of no
     sequence are left as they are in ``out`` (None: a new tensor, which holds anything there)."""
     device = cache.device
-    n, heads, dim = shape = _rows3(q, "q", cache.dtype, device)
+    shape, q_stride = _rows3(q, "q", cache.dtype, device)
+    n, heads, dim = shape
     if dim != cache.head_dim:
         _refuse("q: another head size than the cache's")
-    if page_table.dim() != 2 or page_table.dtype is not _int32() or not page_table.is_cuda or page_table.get_device() != device \
-            or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+    table_shape, table_stride = page_table.shape, page_table.stride()
+    if page_table.dtype is not _rt[4] or page_table.get_device() != device or len(table_shape) != 2 or (table_shape[1] > 1 and table_stride[1] != 1):
         _refuse(f"page_table: need int32 rows [seqs, max_pages] on cuda:{device}")
-    seqs, pages = page_table.shape
+    seqs, pages = table_shape
     lens = _ints(kv_len, "kv_len", (seqs,), device)
     start = _ints(q_start, "q_start", (seqs + 1,), device) if q_start is not None else None
-    if out is None:
-        out = q.new_empty(shape)
-    elif _rows3(out, "out", cache.dtype, device) != shape:
-        _refuse("out: need the shape of q")
-    a = SjdKv4Attention(q.data_ptr(), out.data_ptr(), q.stride(0), out.stride(0), page_table.stride(0), start, lens, page_table.data_ptr(),
+    out, out_stride = _into(out, q, shape, cache.dtype, "out", device)
+    a = SjdKv4Attention(q.data_ptr(), out.data_ptr(), q_stride, out_stride, table_stride[0], start, lens, page_table.data_ptr(),
                         seqs, heads, n, pages, max_q, pages * KV4_PAGE if max_kv is None else max_kv, 1 if causal else 0, skip_nearest,
                         window, dim ** -0.5 if scale is None else scale, None, 0)
-    lib = load_library()
+    lib = _rt[0]
     address, need = C.addressof(a), C.c_size_t()
     rc = lib.sjd_kv4_attention_workspace(cache.address, address, C.addressof(need))
     if rc:
