@@ -83,11 +83,14 @@ __device__ __forceinline__ void seen(const Kv4Attn &a, const Seq &s, int i, int 
 constexpr int kRows = 16;
 constexpr float kLag = 8.f;                       // base 2
 
+// the new token of a row (rows are the query heads of a key head, token by token)
+__device__ __forceinline__ int token_of(const Kv4Attn &a, int row) { return a.group_magic ? (int)__umulhi((uint32_t)row, a.group_magic) : row; }
+
 struct Tile { int first_lo, last_lo, first_hi, last_hi; };      // what the tile's first and last row see
-__device__ __forceinline__ Tile tile_range(const Kv4Attn &a, const Seq &s, int r0, int n_r, int G) {
+__device__ __forceinline__ Tile tile_range(const Kv4Attn &a, const Seq &s, int r0, int n_r) {
     Tile t;
-    seen(a, s, r0 / G, t.first_lo, t.last_lo);
-    seen(a, s, (min(r0 + a.tile, n_r) - 1) / G, t.first_hi, t.last_hi);
+    seen(a, s, token_of(a, r0), t.first_lo, t.last_lo);
+    seen(a, s, token_of(a, min(r0 + a.tile, n_r) - 1), t.first_hi, t.last_hi);
     return t;
 }
 
@@ -137,7 +140,7 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void unroll(F
 }
 
 template <typename T, int NG, int NT>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 || NG > 4 || NT * NG > 4 ? 2 : 3) void kv4_attention_kernel(Kv4Attn a, int n_tiles) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 || NG > 4 || NT * NG > 4 ? 2 : NT == 1 && NG <= 2 ? 5 : 3) void kv4_attention_kernel(Kv4Attn a) {
     typedef typename Op<T>::t HT;
     typedef typename Half16<HT>::v8 v8;
     typedef T qv8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
@@ -146,21 +149,20 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
     __shared__ __attribute__((aligned(16))) float acc[4][kRows * LD];
     __shared__ float ms[4][kRows], ls[4][kRows];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
-    const int G = a.n_heads / a.cache.n_heads;
+    const int G = a.group;
     // pieces further back come last: only long sequences have them
-    const int n_pairs = a.n_seqs * a.cache.n_heads, tile = blockIdx.x % n_tiles, pair = blockIdx.x / n_tiles % n_pairs, part = blockIdx.x / n_tiles / n_pairs;
-    const int b = pair / a.cache.n_heads, h = pair % a.cache.n_heads;
+    const int h = blockIdx.x, b = blockIdx.y, part = a.n_tiles == 1 ? blockIdx.z : blockIdx.z / a.n_tiles, tile = blockIdx.z - part * a.n_tiles;
     const Seq sq = sequence(a, b);
     const int n_r = sq.n * G, r0 = tile * (kRows * NT);
     if (r0 >= n_r) return;
-    const Tile tr = tile_range(a, sq, r0, n_r, G);
+    const Tile tr = tile_range(a, sq, r0, n_r);
     const int lo = tr.first_lo, hi = tr.last_hi;
     const int p0 = max(lo / kKv4Page, part * a.split_pages);
     const int p1 = min(hi < lo ? 0 : hi / kKv4Page + 1, (part + 1) * a.split_pages);
     if (p0 >= p1 && a.n_splits > 1) return;
     int first[NT], last[NT];                      // what row r0 + 16 n + r sees
 #pragma unroll
-    for (int n = 0; n < NT; ++n) seen(a, sq, min(r0 + kRows * n + r, n_r - 1) / G, first[n], last[n]);
+    for (int n = 0; n < NT; ++n) seen(a, sq, token_of(a, min(r0 + kRows * n + r, n_r - 1)), first[n], last[n]);
 
     // The wave's pages (every fourth of the piece): first those that every row sees whole, f0 .. f1 - 1, then the ones after and before.
     const int f0 = min(max((tr.first_hi + kKv4Page - 1) / kKv4Page, p0), p1), f1 = max(min((tr.last_lo + 1) / kKv4Page, p1), f0);
@@ -186,8 +188,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
     v8 qf[NT][NG][NP];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const int row = min(r0 + kRows * n + r, n_r - 1);
-        const T *q = (const T *)a.q + (int64_t)(sq.row0 + row / G) * a.q_stride + (int64_t)(h * G + row % G) * DIM;
+        const int row = min(r0 + kRows * n + r, n_r - 1), tok = token_of(a, row);
+        const T *q = (const T *)a.q + (int64_t)(sq.row0 + tok) * a.q_stride + (int64_t)(h * G + row - tok * G) * DIM;
 #pragma unroll
         for (int s = 0; s < NG; ++s) {
             const qv8 x = *reinterpret_cast<const qv8 *>(q + 8 * (j * NG + s));
@@ -366,8 +368,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
         const float ln = row_sum(l[n]);
         if (j == 0) { ms[wave][r] = m[n]; ls[wave][r] = ln; }
         const bool live = rn + orow < n_r;
-        const int64_t at = sq.row0 + (rn + orow) / G;
-        const int head = h * G + (rn + orow) % G;
+        const int tok = token_of(a, rn + orow), head = h * G + rn + orow - tok * G;
+        const int64_t at = sq.row0 + tok;
 #pragma unroll
         for (int g0 = 0; g0 < NG; g0 += RG) {
             if (g0) __syncthreads();
@@ -413,14 +415,14 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
     constexpr int DIM = 32 * NG, PER = 2 * NG, AHEAD = NG > 4 ? 4 : 8, LANES = WIDE ? 64 : 16, WAYS = LANES / 16;
     typedef T tv __attribute__((ext_vector_type(PER), aligned(sizeof(T))));
     typedef float fv __attribute__((ext_vector_type(PER), aligned(8)));
-    const int G = a.n_heads / a.cache.n_heads, c = threadIdx.x & 15, way = (threadIdx.x & (LANES - 1)) >> 4;
+    const int G = a.group, c = threadIdx.x & 15, way = (threadIdx.x & (LANES - 1)) >> 4;
     const int64_t id = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     const int head = (int)(id % a.n_heads), i = (int)(id / a.n_heads % a.max_q);
     const int64_t b = id / a.n_heads / a.max_q;
     if (b >= a.n_seqs) return;
     const Seq sq = sequence(a, (int)b);
     if (i >= sq.n) return;
-    const Tile tr = tile_range(a, sq, (i * G + head % G) / a.tile * a.tile, sq.n * G, G);
+    const Tile tr = tile_range(a, sq, (i * G + head % G) / a.tile * a.tile, sq.n * G);
     const int lo = tr.first_lo, hi = tr.last_hi;
     const int s0 = lo / kKv4Page / a.split_pages, s1 = hi < lo ? s0 : hi / kKv4Page / a.split_pages + 1;      // the pieces that have been written
     const int64_t at = sq.row0 + i, piece0 = (at * a.n_heads + head) * a.n_splits;
@@ -460,12 +462,12 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
     *reinterpret_cast<tv *>((T *)a.o + at * a.o_stride + (int64_t)head * DIM + c * PER) = out;
 }
 
-int row_tiles(const Kv4Attn &a) { return (int)(((int64_t)a.max_q * (a.n_heads / a.cache.n_heads) + a.tile - 1) / a.tile); }
-
 }  // namespace
 
-void kv4_attention_plan(Kv4Attn &a, bool is_f32) {
-    const int64_t rows = (int64_t)a.max_q * (a.n_heads / a.cache.n_heads);
+bool kv4_attention_plan(Kv4Attn &a, bool is_f32) {
+    a.group = a.n_heads / a.cache.n_heads;
+    a.group_magic = a.group > 1 ? (uint32_t)(((1ull << 32) + a.group - 1) / a.group) : 0u;
+    const int64_t rows = (int64_t)a.max_q * a.group;
     const int pages = (a.max_kv + kKv4Page - 1) / kKv4Page;
     // 32 rows a workgroup share the conversions of a page (8 sequences of 4000 keys, 8 key heads of 64, 1200 rows each: 156 us with 16 rows, 129
     // with 32), but a short launch is over sooner on 16 (one sequence of 1000 keys, 24 rows: 9.0 us, 10.4 with 32).  Registers hold two
@@ -474,7 +476,10 @@ void kv4_attention_plan(Kv4Attn &a, bool is_f32) {
     a.tile = rows > kRows && !is_f32 && a.cache.dim <= 128 && n_pairs * pages >= 256 ? 2 * kRows : kRows;
     // Pieces: workgroups for the chip a few times over (16 sequences of 20000 to 65536 keys, 8 key heads of 128: 1024 workgroups 171 us, 2048 148,
     // 4096 152 and a longer join); fewer of 32 rows, whose sums take longer to write and join than a few pages to read.
-    const int64_t have = n_pairs * row_tiles(a), aim = a.tile == kRows ? 2048 : 1024;
+    a.n_tiles = (int)((rows + a.tile - 1) / a.tile);
+    // workgroups with rows: sequences share n_rows between them
+    const int64_t shared = (int64_t)a.cache.n_heads * ((int64_t)a.n_rows * a.group / a.tile + a.n_seqs), have = n_pairs * a.n_tiles < shared ? n_pairs * a.n_tiles : shared;
+    const int64_t aim = a.tile == kRows ? 2048 : 1024;
     int64_t want = have ? (aim + have - 1) / have : 1;
     want = want < 1 ? 1 : want;
     int per = (int)((pages + want - 1) / want);
@@ -482,10 +487,9 @@ void kv4_attention_plan(Kv4Attn &a, bool is_f32) {
     a.split_pages = per < 4 ? 4 : per;
     a.n_splits = (pages + a.split_pages - 1) / a.split_pages;
     if (a.n_splits < 1) a.n_splits = 1;
-}
-
-int64_t kv4_attention_grid(const Kv4Attn &a) {
-    return (int64_t)a.n_seqs * a.cache.n_heads * row_tiles(a) * a.n_splits;
+    // the grid's second and third dimension, and rows for which group_magic is exact
+    return a.n_seqs <= 65535 && (int64_t)a.n_tiles * a.n_splits <= 65535 && rows * a.group < (int64_t)1 << 31 &&
+           (int64_t)a.n_seqs * a.n_heads * a.max_q <= INT32_MAX;
 }
 
 size_t kv4_attention_workspace(const Kv4Attn &a) {
@@ -493,12 +497,10 @@ size_t kv4_attention_workspace(const Kv4Attn &a) {
 }
 
 template <typename T> void launch_kv4_attention(const Kv4Attn &a, hipStream_t s) {
-    const int n_tiles = row_tiles(a);
-    const int64_t n = kv4_attention_grid(a);
-    if (n <= 0 || a.n_rows <= 0) return;
-    const dim3 grid((unsigned)n), block(256);
+    if (a.n_rows <= 0 || a.n_seqs <= 0 || a.n_tiles <= 0) return;
+    const dim3 grid(a.cache.n_heads, a.n_seqs, a.n_tiles * a.n_splits), block(256);
     const int nt = a.tile / kRows;
-#define SJD_KV4_ATTEND(NG, NT) hipLaunchKernelGGL((kv4_attention_kernel<T, NG, NT>), grid, block, 0, s, a, n_tiles)
+#define SJD_KV4_ATTEND(NG, NT) hipLaunchKernelGGL((kv4_attention_kernel<T, NG, NT>), grid, block, 0, s, a)
     if constexpr (sizeof(T) == 4) {
         switch (a.cache.dim / 32) {
             case 1: SJD_KV4_ATTEND(1, 1); break;

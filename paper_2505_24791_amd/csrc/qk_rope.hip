@@ -157,39 +157,37 @@ template <typename T> __device__ __forceinline__ void hold_value(uint8_t *b, int
 
 constexpr int kThreads = 256;
 
-// A workgroup takes `per` rows: cos and sin of every (row, pair) once for all heads, through LDS, then L lanes a head, eight channels each, the
-// next head's row requested under the present one's arithmetic.  WRITE: rounded keys go to LDS instead of memory, and with the values from
-// there into the cache.
-struct RopeShape { int per; uint32_t magic; double per_dim; };      // magic: n / heads = n * magic >> 32 for the n of a workgroup
+// A workgroup takes `per` rows, a power of two; L lanes (a group) take a head, eight channels each.  A group keeps its row and goes over every
+// `step`-th head of it, so that addresses move by constants; the next head is requested under the present one's arithmetic.  cos and sin of every
+// (row, pair) are made once for all heads, in LDS.  WRITE: rounded keys go to LDS instead of memory, and with the values from there into
+// the cache.
+struct RopeShape { int per, log_step; double per_dim; };
 
 template <typename T, int L, bool WRITE>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kernel(QkOpts o, QkRows r, Kv4Cache c, RopeShape sh) {
+__global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 5) void qk_rope_kernel(QkOpts o, QkRows r, Kv4Cache c, RopeShape sh) {
     typedef typename Vec<T, 4>::v v4;
     typedef typename Vec<T, 8>::v v8;
-    constexpr int SLOTS = kThreads / L;
     extern __shared__ __attribute__((aligned(16))) char smem[];
-    const int pairs = o.rot / 2;
-    double2 *cs = reinterpret_cast<double2 *>(smem);                                     // [per][4][pairs / 4]: a lane's four pairs apart, or neighbouring lanes meet in a bank
-    float *affine = reinterpret_cast<float *>(smem + (size_t)sh.per * pairs * sizeof(double2));   // [4][dim] gains of q and k, shifts of q and k
+    const int pairs = o.rot / 2, quads = pairs / 4;
+    double2 *cs = reinterpret_cast<double2 *>(smem);                                     // [per][4][quads]: a lane's four pairs apart, or neighbouring lanes meet in a bank
+    float *affine = reinterpret_cast<float *>(cs + (size_t)sh.per * pairs);              // [4][dim] gains of q and k, shifts of q and k
     T *keys = reinterpret_cast<T *>(affine + 4 * r.dim);                                 // [per][n_kv][dim]
-    const int tid = threadIdx.x, i = tid % L, row0 = blockIdx.x * sh.per, rows = min(sh.per, r.n_rows - row0);
-    const int n_q = r.q ? r.n_heads : 0, heads = n_q + (r.k ? r.n_kv : 0), n = rows * heads;
+    const int tid = threadIdx.x, i = tid % L, group = tid / L, row0 = blockIdx.x * sh.per, rows = min(sh.per, r.n_rows - row0);
+    const int step = 1 << sh.log_step, row = group >> sh.log_step, h0 = group & (step - 1);
+    const int n_q = r.q ? r.n_heads : 0, n_k = r.k ? r.n_kv : 0;
+    const int k0 = (unsigned)(h0 + (step - 1) * n_q) % (unsigned)step;                   // (h0 - n_q) mod step: groups that have no query head left begin with keys
     const Pieces p = pieces(i, o);
-    const bool live = 8 * i < r.dim, turns = 8 * i < o.rot, shifted = o.q_shift || o.k_shift;
-    v4 xa = {}, xb = {};                       // lanes past the head keep zeros
-    auto split = [&](int t, int &row, int &h) {
-        row = heads == 1 ? t : (int)__umulhi((uint32_t)t, sh.magic);
-        h = t - row * heads;
+    const bool there = row < rows, live = 8 * i < r.dim && there, turning = 8 * i < o.rot;
+    const int64_t at = row0 + row;
+
+    auto fetch = [&](const T *x, v4 &a, v4 &b) {
+        a = *reinterpret_cast<const v4 *>(x + p.a);
+        b = *reinterpret_cast<const v4 *>(x + p.b);
     };
-    auto fetch = [&](int t) {
-        if (t >= n || !live) return;
-        int row, h;
-        split(t, row, h);
-        const T *x = h < n_q ? (const T *)r.q + (row0 + row) * r.q_stride + h * r.dim : (const T *)r.k + (row0 + row) * r.k_stride + (h - n_q) * r.dim;
-        xa = *reinterpret_cast<const v4 *>(x + p.a);
-        xb = *reinterpret_cast<const v4 *>(x + p.b);
-    };
-    fetch(tid / L);
+    const T *qx = (const T *)r.q + at * r.q_stride + (int64_t)h0 * r.dim, *kx = (const T *)r.k + at * r.k_stride + (int64_t)k0 * r.dim;
+    v4 qa = {}, qb = {}, ka = {}, kb = {};     // lanes past the head keep zeros
+    if (live && h0 < n_q) fetch(qx, qa, qb);
+    if (live && k0 < n_k) fetch(kx, ka, kb);
     if (o.norm)
         for (int e = tid; e < r.dim; e += kThreads) {
             affine[e] = o.q_gain ? o.q_gain[e] : 1.f;
@@ -198,94 +196,96 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 6) void qk_rope_kern
             affine[3 * r.dim + e] = o.k_shift ? o.k_shift[e] : 0.f;
         }
     for (int t = tid; t < rows * pairs; t += kThreads) {
-        const int row = t / pairs, pi = t - row * pairs;
+        const int tr = t / pairs, pi = t - tr * pairs;
         int axis = 0;
         while (axis + 1 < o.n_axes && pi >= o.axis_end[axis]) ++axis;
-        cs[row * pairs + (pi & 3) * (pairs / 4) + pi / 4] = unit(r.pos[(int64_t)(row0 + row) * o.n_axes + axis], o.freq[pi]);
+        cs[tr * pairs + (pi & 3) * quads + pi / 4] = unit(r.pos[(int64_t)(row0 + tr) * o.n_axes + axis], o.freq[pi]);
     }
     __syncthreads();
-    for (int t = tid / L; t < n; t += SLOTS) {
-        int row, h;
-        split(t, row, h);
-        const bool is_q = h < n_q;
-        double y[8];
+    const double2 *turns = cs + row * pairs + i;
+    auto walk = [&](int h, int heads, const T *x, T *out, const float *gain, bool shifted, v4 a, v4 b) {
+        const int64_t hop = (int64_t)step * r.dim;
+        for (; h < heads; h += step) {
+            asm volatile("" ::: "memory");       // factors are read from LDS for each head: kept in registers they would halve the waves
+            double y[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            y[e] = (double)to_f32<T>(xa[e]);
-            y[4 + e] = (double)to_f32<T>(xb[e]);
-        }
-        fetch(t + SLOTS);
-        if (o.norm) {
-            if (o.norm == 2) {
+            for (int e = 0; e < 4; ++e) {
+                y[e] = (double)to_f32<T>(a[e]);
+                y[4 + e] = (double)to_f32<T>(b[e]);
+            }
+            x += hop;
+            if (live && h + step < heads) fetch(x, a, b);
+            if (o.norm) {
+                if (o.norm == 2) {
+                    double s = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) s += y[e];
+                    const double mean = lanes_sum<L>(s) * sh.per_dim;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = live ? y[e] - mean : 0.0;
+                }
                 double s = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) s += y[e];
-                const double mean = lanes_sum<L>(s) * sh.per_dim;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = live ? y[e] - mean : 0.0;
-            }
-            double s = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s = fma(y[e], y[e], s);
-            const double n_inv = rsqrt(fma(lanes_sum<L>(s), sh.per_dim, (double)o.eps));
-            const float *g = affine + (is_q ? 0 : r.dim);
-            if (live) {
-                const f32x4 ga = *reinterpret_cast<const f32x4 *>(g + p.a), gb = *reinterpret_cast<const f32x4 *>(g + p.b);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    y[e] *= n_inv * (double)ga[e];
-                    y[4 + e] *= n_inv * (double)gb[e];
-                }
-                if (shifted) {
-                    const f32x4 sa = *reinterpret_cast<const f32x4 *>(g + 2 * r.dim + p.a), sb = *reinterpret_cast<const f32x4 *>(g + 2 * r.dim + p.b);
+                for (int e = 0; e < 8; ++e) s = fma(y[e], y[e], s);
+                const double n_inv = rsqrt(fma(lanes_sum<L>(s), sh.per_dim, (double)o.eps));
+                if (live) {
+                    const f32x4 ga = *reinterpret_cast<const f32x4 *>(gain + p.a), gb = *reinterpret_cast<const f32x4 *>(gain + p.b);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        y[e] += (double)sa[e];
-                        y[4 + e] += (double)sb[e];
+                        y[e] *= n_inv * (double)ga[e];
+                        y[4 + e] *= n_inv * (double)gb[e];
+                    }
+                    if (shifted) {
+                        const f32x4 sa = *reinterpret_cast<const f32x4 *>(gain + 2 * r.dim + p.a), sb = *reinterpret_cast<const f32x4 *>(gain + 2 * r.dim + p.b);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            y[e] += (double)sa[e];
+                            y[4 + e] += (double)sb[e];
+                        }
                     }
                 }
             }
-        }
-        if (!live) continue;
-        if (turns) {
-            const double2 *u = cs + row * pairs + i;
-            if (o.adjacent) {
+            if (!live) continue;
+            if (turning) {
+                if (o.adjacent) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) turn(y[2 * e], y[2 * e + 1], u[e * (pairs / 4)]);
-            } else {
+                    for (int e = 0; e < 4; ++e) turn(y[2 * e], y[2 * e + 1], turns[e * quads]);
+                } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) turn(y[e], y[4 + e], u[e * (pairs / 4)]);
+                    for (int e = 0; e < 4; ++e) turn(y[e], y[4 + e], turns[e * quads]);
+                }
             }
+            store4<T>(out + p.a, y);
+            store4<T>(out + p.b, y + 4);
+            out += hop;
         }
-        T *out = is_q ? (T *)r.q_out + (row0 + row) * r.q_out_stride + h * r.dim
-               : WRITE ? keys + ((size_t)row * r.n_kv + h - n_q) * r.dim : (T *)r.k_out + (row0 + row) * r.k_out_stride + (h - n_q) * r.dim;
-        store4<T>(out + p.a, y);
-        store4<T>(out + p.b, y + 4);
-    }
-    if constexpr (WRITE) {
-        constexpr int AHEAD = 4;                            // values requested before the first is needed
-        const int n_v = rows * r.n_kv;
+    };
+    walk(h0, n_q, qx, (T *)r.q_out + at * r.q_out_stride + (int64_t)h0 * r.dim, affine, o.q_shift, qa, qb);
+    if constexpr (!WRITE) {
+        walk(k0, n_k, kx, (T *)r.k_out + at * r.k_out_stride + (int64_t)k0 * r.dim, affine + r.dim, o.k_shift, ka, kb);
+    } else {
+        walk(k0, n_k, kx, keys + ((int64_t)row * r.n_kv + k0) * r.dim, affine + r.dim, o.k_shift, ka, kb);
+        constexpr int AHEAD = 4;                // values requested before the first is needed
+        const T *vx = (const T *)r.v + at * r.v_stride + (int64_t)h0 * r.dim + 8 * i;
         v8 xv[AHEAD];
-        auto fetch_v = [&](int u, int t) {
-            if (t >= n_v) return;
-            const int row = t / r.n_kv, h = t - row * r.n_kv;
-            xv[u] = *reinterpret_cast<const v8 *>((const T *)r.v + (row0 + row) * r.v_stride + h * r.dim + 8 * i);
-        };
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) fetch_v(u, tid / L + u * SLOTS);
+        for (int w = 0; w < AHEAD; ++w)
+            if (there && h0 + w * step < n_k) xv[w] = *reinterpret_cast<const v8 *>(vx + w * step * r.dim);
+        const int32_t slot = there ? r.slot[at] : -1;
+        const int off = slot & (kKv4Page - 1);
         __syncthreads();
-        for (int t0 = tid / L; t0 < n_v; t0 += AHEAD * SLOTS)
+        if (!there) return;
+        uint8_t *blk = block_of(c, slot, h0);
+        const T *key = keys + ((int64_t)row * r.n_kv + h0) * r.dim + 8 * i;
+        for (int h = h0; h < n_k; h += AHEAD * step)
 #pragma unroll
-            for (int u = 0; u < AHEAD; ++u) {
-                const int t = t0 + u * SLOTS;
-                if (t >= n_v) break;
-                const int row = t / r.n_kv, h = t - row * r.n_kv;
-                const int32_t slot = r.slot[row0 + row];
-                uint8_t *b = block_of(c, slot, h);
-                const int off = slot & (kKv4Page - 1);
-                hold_value<T>(b, r.dim, off, i, xv[u]);
-                fetch_v(u, t + AHEAD * SLOTS);
-                hold_key<T>(b, r.dim, off, i, *reinterpret_cast<const v8 *>(keys + (size_t)t * r.dim + 8 * i));
+            for (int w = 0; w < AHEAD; ++w) {
+                if (h + w * step >= n_k) break;
+                hold_value<T>(blk, r.dim, off, i, xv[w]);
+                if (h + (w + AHEAD) * step < n_k) xv[w] = *reinterpret_cast<const v8 *>(vx + (int64_t)(h - h0 + (w + AHEAD) * step) * r.dim);
+                hold_key<T>(blk, r.dim, off, i, *reinterpret_cast<const v8 *>(key));
+                if (blk) blk += (size_t)step * kv4_block_bytes(r.dim);
+                key += step * r.dim;
             }
     }
 }
@@ -342,19 +342,17 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4Cache c, const in
 }
 
 template <typename T, int L, bool WRITE>
-void launch_rope_lanes(const QkOpts &o, QkRows r, const Kv4Cache &c, hipStream_t s) {
-    if (!r.q) r.n_heads = 0;
-    if (!r.k) r.n_kv = 0;
+void launch_rope_lanes(const QkOpts &o, const QkRows &r, const Kv4Cache &c, hipStream_t s) {
     constexpr int GROUPS = kThreads / L;
-    const int heads = r.n_heads + r.n_kv;
-    // Rows of a workgroup: eight heads for a lane group, but 1024 workgroups where there are rows enough, and LDS that lets six share a CU
-    const size_t row_lds = (size_t)(o.rot / 2) * sizeof(double2) + (WRITE ? (size_t)r.n_kv * r.dim * sizeof(T) : 0), affine = 4 * r.dim * sizeof(float);
-    int per = 8 * GROUPS / heads;
-    if (per > r.n_rows / 1024) per = r.n_rows / 1024;
-    while (per > 1 && per * row_lds + affine > 26624) per /= 2;
-    if (per < 1) per = 1;
-    const RopeShape sh{per, heads > 1 ? (uint32_t)(((1ull << 32) + heads - 1) / heads) : 0u, 1.0 / r.dim};
-    hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE>), dim3((r.n_rows + per - 1) / per), dim3(kThreads), per * row_lds + affine, s, o, r, c, sh);
+    const int heads = (r.q ? r.n_heads : 0) + (r.k ? r.n_kv : 0);
+    // Rows of a workgroup: eight heads for a group, but 1024 workgroups where there are rows enough, and LDS that lets five share a CU
+    const size_t row_lds = (size_t)(o.rot / 2) * sizeof(double2) + (WRITE ? (size_t)r.n_kv * r.dim * sizeof(T) : 0);
+    int per = GROUPS;
+    while (per > 1 && (per * heads > 8 * GROUPS || per > r.n_rows / 1024 || per * row_lds > 28672)) per /= 2;
+    int log_step = 0;
+    while (per << log_step < GROUPS) ++log_step;
+    const RopeShape sh{per, log_step, 1.0 / r.dim};
+    hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE>), dim3((r.n_rows + per - 1) / per), dim3(kThreads), per * row_lds + 4 * r.dim * sizeof(float), s, o, r, c, sh);
 }
 
 template <typename T, bool WRITE>

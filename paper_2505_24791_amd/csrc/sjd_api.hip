@@ -1582,8 +1582,7 @@ int check_attention(const sjd_kv4 *c, const sjd_kv4_attention *g, Kv4Attn *out) 
     a.max_kv = (int)((int64_t)g->max_pages * SJD_KV4_PAGE < g->max_kv ? (int64_t)g->max_pages * SJD_KV4_PAGE : g->max_kv);
     a.causal = g->causal != 0; a.skip = g->skip_nearest; a.window = g->window;
     a.scale_log2 = g->scale * 1.44269504088896340736f;
-    kv4_attention_plan(a, c->dtype == SJD_DTYPE_F32);
-    if (kv4_attention_grid(a) > INT32_MAX) return fail(SJD_EINVAL, "too many rows and sequences for one call");
+    if (!kv4_attention_plan(a, c->dtype == SJD_DTYPE_F32)) return fail(SJD_EINVAL, "too many rows or sequences for one call");
     *out = a;
     return SJD_OK;
 }
