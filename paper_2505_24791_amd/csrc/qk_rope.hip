@@ -307,37 +307,48 @@ __global__ __launch_bounds__(kThreads) void kv4_write_kernel(QkRows r, Kv4Cache 
     hold_value<T>(b, r.dim, slot & (kKv4Page - 1), ch, v);
 }
 
-// eight channels a lane: of the keys of a token, then of its values; zeros for a slot outside the cache
+// Eight channels a thread, of a token's key and of its value; zeros for a slot outside the cache.  A workgroup takes one head of rows that follow
+// one another: where these are a page's tokens it reads the head's block of the page whole, which workgroups on other XCDs would otherwise read
+// again into their L2 (40000 tokens of 16 heads of 64, cold: 60 us with two rows of all heads a workgroup).
+constexpr int kReadAhead = 2;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4Cache c, const int32_t *slots, T *k, int64_t k_stride, T *v, int64_t v_stride,
                                                             int n_rows) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
-    const int chunks = c.dim / 8;
-    const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int64_t row = id / (c.n_heads * chunks);
-    if (row >= n_rows) return;
-    const int rest = (int)(id - row * c.n_heads * chunks), h = rest / chunks, ch = rest - h * chunks;
-    const int32_t slot = slots[row];
-    const uint8_t *b = block_of(c, slot, h);
-    const int off = slot % kKv4Page;
-    uint32_t w[2] = {0, 0}, sb[2] = {0, 0};
-    if (b) {
-        w[0] = *reinterpret_cast<const uint32_t *>(b + kv4_k_code(c.dim, off, ch));
-        sb[0] = b[kv4_k_scale(c.dim, off, ch / 4)];
-        for (int q = 0; q < 4; ++q) w[1] |= (uint32_t)b[kv4_v_code(c.dim, off, 4 * (ch % 4) + q) + ch / 4] << (8 * q);
-        sb[1] = b[kv4_v_scale(c.dim, off) + ch / 4];
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    const int chunks = c.dim / 8, ng = c.dim / 32, h = blockIdx.y, ch = threadIdx.x % chunks, rows = kThreads / chunks;
+    const int64_t row0 = (int64_t)blockIdx.x * rows * kReadAhead + threadIdx.x / chunks;
+    uint32_t w[kReadAhead][2], sb[kReadAhead][2];
+#pragma unroll
+    for (int u = 0; u < kReadAhead; ++u) {
+        const int64_t row = row0 + u * rows;
+        const int32_t slot = row < n_rows ? slots[row] : -1;
+        const uint8_t *b = block_of(c, slot, h);
+        const int off = slot & (kKv4Page - 1);
+        w[u][0] = w[u][1] = sb[u][0] = sb[u][1] = 0;
+        if (b) {
+            w[u][0] = *reinterpret_cast<const uint32_t *>(b + kv4_k_code(c.dim, off, ch));
+            sb[u][0] = b[kv4_k_scale(c.dim, off, ch / 4)];
+            const uint8_t *vb = b + kv4_v_code(c.dim, off, 4 * (ch % 4)) + ch / 4;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[u][1] |= (uint32_t)vb[q * 4 * ng] << (8 * q);
+            sb[u][1] = b[kv4_v_scale(c.dim, off) + ch / 4];
+        }
     }
-    T *out[2] = {k + row * k_stride + (int64_t)h * c.dim + 8 * ch, v + row * v_stride + (int64_t)h * c.dim + 8 * ch};
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-        const float s = scale_of(sb[z]);
-        f32x2 x[4];
-        x[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[z], s, 0);
-        x[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[z], s, 1);
-        x[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[z], s, 2);
-        x[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[z], s, 3);
+    for (int u = 0; u < kReadAhead; ++u) {
+        const int64_t row = row0 + u * rows;
+        if (row >= n_rows) return;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) out[z][e] = from_f32<T>(x[e / 2][e % 2]);
+        for (int z = 0; z < 2; ++z) {
+            const float s = scale_of(sb[u][z]);
+            const t2 x0 = __builtin_convertvector((f32x2)__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u][z], s, 0), t2);
+            const t2 x1 = __builtin_convertvector((f32x2)__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u][z], s, 1), t2);
+            const t2 x2 = __builtin_convertvector((f32x2)__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u][z], s, 2), t2);
+            const t2 x3 = __builtin_convertvector((f32x2)__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u][z], s, 3), t2);
+            T *out = (z ? v + row * v_stride : k + row * k_stride) + (int64_t)h * c.dim + 8 * ch;
+            *reinterpret_cast<typename Vec<T, 8>::v *>(out) = typename Vec<T, 8>::v{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+        }
     }
 }
 
@@ -379,8 +390,9 @@ template <typename T> void launch_kv4_write(const Kv4Cache &c, const QkOpts *o, 
 template <typename T> void launch_kv4_read(const Kv4Cache &c, const int32_t *slot, void *k, int64_t k_stride, void *v, int64_t v_stride,
                                            int n_rows, hipStream_t s) {
     if (n_rows <= 0) return;
-    const int64_t n = ((int64_t)n_rows * c.n_heads * (c.dim / 8) + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL((kv4_read_kernel<T>), dim3((unsigned)n), dim3(kThreads), 0, s, c, slot, (T *)k, k_stride, (T *)v, v_stride, n_rows);
+    const int rows = kThreads / (c.dim / 8) * kReadAhead;
+    hipLaunchKernelGGL((kv4_read_kernel<T>), dim3((n_rows + rows - 1) / rows, c.n_heads), dim3(kThreads), 0, s, c, slot, (T *)k, k_stride,
+                       (T *)v, v_stride, n_rows);
 }
 
 #define SJD_KV4_ROWS(T)                                                                                     \
