@@ -9,6 +9,8 @@
 // of float32 here, and these kernels move bytes: each row is read once and written once.
 #include "kv4.h"
 
+#include <type_traits>
+
 namespace sjd {
 
 namespace {
@@ -75,12 +77,21 @@ __device__ __forceinline__ void turn(double &a, double &b, double2 u) {
 template <typename T, int N> struct Vec { typedef T v __attribute__((ext_vector_type(N), aligned(sizeof(T)))); };
 
 // Through float32, kept apart: in one step the compiler rounds float64 to 16 bits with thirty instructions of its own.
-template <typename T> __device__ __forceinline__ void store4(T *p, const double *y) {
+template <typename T> __device__ __forceinline__ typename Vec<T, 4>::v round4(const double *y) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     typedef T t2 __attribute__((ext_vector_type(2)));
     const t2 a = __builtin_convertvector((f32x2{keep_f32((float)y[0]), keep_f32((float)y[1])}), t2);
     const t2 b = __builtin_convertvector((f32x2{keep_f32((float)y[2]), keep_f32((float)y[3])}), t2);
-    *reinterpret_cast<typename Vec<T, 4>::v *>(p) = typename Vec<T, 4>::v{a[0], a[1], b[0], b[1]};
+    return typename Vec<T, 4>::v{a[0], a[1], b[0], b[1]};
+}
+
+// Results of more than what the L2 caches hold (4 MB on each XCD) are stored past them: cold, 40000 tokens of 16 heads of 64 are read back in 32 us
+// that way and 53 through the caches, 32768 rows of 2 x 16 heads of 64 turned in 57 and 59.  Smaller ones stay for the call that comes next.
+constexpr int64_t kStreamBytes = 32 << 20;
+template <typename T, int N, bool STREAM> __device__ __forceinline__ void store(T *p, typename Vec<T, N>::v v) {
+    typename Vec<T, N>::v *d = reinterpret_cast<typename Vec<T, N>::v *>(p);
+    if constexpr (STREAM) __builtin_nontemporal_store(v, d);
+    else *d = v;
 }
 
 // Where a lane's two pieces of four channels begin: piece b holds the partners of piece a where the pairs are rot / 2 apart.
@@ -163,7 +174,7 @@ constexpr int kThreads = 256;
 // the cache.
 struct RopeShape { int per, log_step; double per_dim; };
 
-template <typename T, int L, bool WRITE>
+template <typename T, int L, bool WRITE, bool STREAM>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 5) void qk_rope_kernel(QkOpts o, QkRows r, Kv4Cache c, RopeShape sh) {
     typedef typename Vec<T, 4>::v v4;
     typedef typename Vec<T, 8>::v v8;
@@ -203,7 +214,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 5) void qk_rope_kern
     }
     __syncthreads();
     const double2 *turns = cs + row * pairs + i;
-    auto walk = [&](int h, int heads, const T *x, T *out, const float *gain, bool shifted, v4 a, v4 b) {
+    auto walk = [&](int h, int heads, const T *x, T *out, const float *gain, bool shifted, auto streamed, v4 a, v4 b) {
         const int64_t hop = (int64_t)step * r.dim;
         for (; h < heads; h += step) {
             asm volatile("" ::: "memory");       // factors are read from LDS for each head: kept in registers they would halve the waves
@@ -255,16 +266,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 5) void qk_rope_kern
                     for (int e = 0; e < 4; ++e) turn(y[e], y[4 + e], turns[e * quads]);
                 }
             }
-            store4<T>(out + p.a, y);
-            store4<T>(out + p.b, y + 4);
+            store<T, 4, decltype(streamed)::value>(out + p.a, round4<T>(y));
+            store<T, 4, decltype(streamed)::value>(out + p.b, round4<T>(y + 4));
             out += hop;
         }
     };
-    walk(h0, n_q, qx, (T *)r.q_out + at * r.q_out_stride + (int64_t)h0 * r.dim, affine, o.q_shift, qa, qb);
+    walk(h0, n_q, qx, (T *)r.q_out + at * r.q_out_stride + (int64_t)h0 * r.dim, affine, o.q_shift, std::bool_constant<STREAM>{}, qa, qb);
     if constexpr (!WRITE) {
-        walk(k0, n_k, kx, (T *)r.k_out + at * r.k_out_stride + (int64_t)k0 * r.dim, affine + r.dim, o.k_shift, ka, kb);
+        walk(k0, n_k, kx, (T *)r.k_out + at * r.k_out_stride + (int64_t)k0 * r.dim, affine + r.dim, o.k_shift, std::bool_constant<STREAM>{}, ka, kb);
     } else {
-        walk(k0, n_k, kx, keys + ((int64_t)row * r.n_kv + k0) * r.dim, affine + r.dim, o.k_shift, ka, kb);
+        walk(k0, n_k, kx, keys + ((int64_t)row * r.n_kv + k0) * r.dim, affine + r.dim, o.k_shift, std::false_type{}, ka, kb);
         constexpr int AHEAD = 4;                // values requested before the first is needed
         const T *vx = (const T *)r.v + at * r.v_stride + (int64_t)h0 * r.dim + 8 * i;
         v8 xv[AHEAD];
@@ -311,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void kv4_write_kernel(QkRows r, Kv4Cache 
 // one another: where these are a page's tokens it reads the head's block of the page whole, which workgroups on other XCDs would otherwise read
 // again into their L2 (40000 tokens of 16 heads of 64, cold: 60 us with two rows of all heads a workgroup).
 constexpr int kReadAhead = 2;
-template <typename T>
+template <typename T, bool STREAM>
 __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4Cache c, const int32_t *slots, T *k, int64_t k_stride, T *v, int64_t v_stride,
                                                             int n_rows) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -347,7 +358,7 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4Cache c, const in
             const t2 x2 = __builtin_convertvector((f32x2)__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u][z], s, 2), t2);
             const t2 x3 = __builtin_convertvector((f32x2)__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u][z], s, 3), t2);
             T *out = (z ? v + row * v_stride : k + row * k_stride) + (int64_t)h * c.dim + 8 * ch;
-            *reinterpret_cast<typename Vec<T, 8>::v *>(out) = typename Vec<T, 8>::v{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+            store<T, 8, STREAM>(out, typename Vec<T, 8>::v{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]});
         }
     }
 }
@@ -362,8 +373,12 @@ void launch_rope_lanes(const QkOpts &o, const QkRows &r, const Kv4Cache &c, hipS
     while (per > 1 && (per * heads > 8 * GROUPS || per > r.n_rows / 1024 || per * row_lds > 28672)) per /= 2;
     int log_step = 0;
     while (per << log_step < GROUPS) ++log_step;
+    const bool stream = (int64_t)r.n_rows * ((r.q ? r.n_heads : 0) + (r.k && !WRITE ? r.n_kv : 0)) * r.dim * (int64_t)sizeof(T) > kStreamBytes;
     const RopeShape sh{per, log_step, 1.0 / r.dim};
-    hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE>), dim3((r.n_rows + per - 1) / per), dim3(kThreads), per * row_lds + 4 * r.dim * sizeof(float), s, o, r, c, sh);
+    const dim3 grid((r.n_rows + per - 1) / per), block(kThreads);
+    const size_t lds = per * row_lds + 4 * r.dim * sizeof(float);
+    if (stream) hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE, true>), grid, block, lds, s, o, r, c, sh);
+    else hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE, false>), grid, block, lds, s, o, r, c, sh);
 }
 
 template <typename T, bool WRITE>
@@ -391,8 +406,11 @@ template <typename T> void launch_kv4_read(const Kv4Cache &c, const int32_t *slo
                                            int n_rows, hipStream_t s) {
     if (n_rows <= 0) return;
     const int rows = kThreads / (c.dim / 8) * kReadAhead;
-    hipLaunchKernelGGL((kv4_read_kernel<T>), dim3((n_rows + rows - 1) / rows, c.n_heads), dim3(kThreads), 0, s, c, slot, (T *)k, k_stride,
-                       (T *)v, v_stride, n_rows);
+    const dim3 grid((n_rows + rows - 1) / rows, c.n_heads), block(kThreads);
+    if (2 * (int64_t)n_rows * c.n_heads * c.dim * (int64_t)sizeof(T) > kStreamBytes)
+        hipLaunchKernelGGL((kv4_read_kernel<T, true>), grid, block, 0, s, c, slot, (T *)k, k_stride, (T *)v, v_stride, n_rows);
+    else
+        hipLaunchKernelGGL((kv4_read_kernel<T, false>), grid, block, 0, s, c, slot, (T *)k, k_stride, (T *)v, v_stride, n_rows);
 }
 
 #define SJD_KV4_ROWS(T)                                                                                     \

@@ -269,6 +269,44 @@ def _check(torch, got, q, q_start, lens, keys, values, name, **kw):
     assert worst <= 1.0, worst
 
 
+@pytest.mark.parametrize("name", TYPES)
+def test_large_calls_give_the_bits_of_small_ones(torch_cuda, name):
+    """Results of some 50 MB, at odd strides, against the same rows in calls of a thousand; padding between the rows stays."""
+    import paper_2505_24791_amd as sjd
+    torch = torch_cuda
+    rng = np.random.default_rng(8)
+    n, H, KV, dim, cut = 10011, 12, 4, 128, 1000
+    dt = getattr(torch, name)
+    qkv = torch.randn((n, (H + 2 * KV) * dim + 3), dtype=torch.float32, device="cuda").to(dt)
+    q, k, v = (qkv[:, 1 + a * dim:1 + b * dim].unflatten(1, (b - a, dim)) for a, b in ((0, H), (H, H + KV), (H + KV, H + 2 * KV)))
+    o, _ = _opts(torch, sjd, rng, dim, "layer", 64, False, (16, 16))
+    pos = torch.from_numpy(rng.integers(0, 5000, (n, 2)).astype(np.int32)).cuda()
+    wide = [torch.full((n, h * dim + 5), 7.0, dtype=dt, device="cuda") for h in (H, KV, H)]
+    qo, ko, qw = (w[:, 3:3 + h * dim].unflatten(1, (h, dim)) for w, h in zip(wide, (H, KV, H)))
+    slot = torch.from_numpy(rng.permutation((n // 64 + 2) * 64)[:n].astype(np.int32)).cuda()
+    sjd.op_qk_norm_rope(q, k, pos, o, q_out=qo, k_out=ko)
+    a, b = (sjd.Kv4Cache.zeros(n // 64 + 2, KV, dim, dt) for _ in range(2))
+    sjd.op_kv4_write(a, k, v, slot, q=q, pos=pos, opts=o, q_out=qw)
+    for i in range(0, n, cut):
+        s = slice(i, i + cut)
+        gq, gk = sjd.op_qk_norm_rope(q[s], k[s], pos[s], o)
+        assert torch.equal(qo[s], gq) and torch.equal(ko[s], gk) and torch.equal(qw[s], gq)
+        sjd.op_kv4_write(b, gk, v[s], slot[s])
+    for w in wide:
+        assert bool((w[:, :3] == 7).all()) and bool((w[:, -2:] == 7).all())
+    assert torch.equal(a.pages, b.pages)
+    kr, vr = (torch.full((n, KV * dim + 1), 7.0, dtype=dt, device="cuda") for _ in range(2))
+    many = slot.repeat(3)
+    gk, gv = sjd.op_kv4_read(a, many)                                                  # 62 MB of 16-bit rows
+    sjd.op_kv4_read(a, slot, k_out=kr[:, 1:].unflatten(1, (KV, dim)), v_out=vr[:, :-1].unflatten(1, (KV, dim)))
+    assert torch.equal(kr[:, 1:].unflatten(1, (KV, dim)), gk[:n]) and bool((kr[:, 0] == 7).all()) and bool((vr[:, -1] == 7).all())
+    for j in range(3):
+        for i in range(0, n, cut):
+            wk, wv = sjd.op_kv4_read(a, slot[i:i + cut])
+            at = slice(j * n + i, j * n + min(i + cut, n))
+            assert torch.equal(gk[at], wk) and torch.equal(gv[at], wv)
+
+
 ATTEND = [
     # kv heads, heads, dim, keys of the sequences, new tokens of them, causal, skip, window
     (2, 2, 64, [1, 64, 65, 200], [1, 1, 1, 1], True, 0, 0),
