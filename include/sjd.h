@@ -266,7 +266,8 @@ SJD_API int sjd_op_attention_h16(int dtype, const void *qkv_dev, void *o_dev, in
  * with gains and shifts [head_dim] float32 (NULL: 1 and 0; they need a norm).  The first rot_dim channels then turn in pairs:
  * pairing 0 takes channels (i, i + rot_dim / 2), pairing 1 takes (2 i, 2 i + 1), i < rot_dim / 2, and pair i turns by
  * position * freq_dev[i] radians, (a, b) -> (a cos - b sin, a sin + b cos).  The pairs are dealt to the axes in order, axis_pairs[a] of
- * them to axis a; each axis has a position of its own (any int32).  Everything in between is computed in float64 and rounded once. */
+ * them to axis a; each axis has a position of its own (any int32; |position * freq| below 2^50).  Everything in between is computed in float64 and
+ * rounded once. */
 typedef struct {
     int32_t norm;                 /* 0, 1, 2 */
     float eps;                    /* >= 0 */
@@ -314,7 +315,8 @@ SJD_API int sjd_op_kv4_read(const sjd_kv4 *cache, const int32_t *slot_dev, void 
  * the cache); q_start_dev NULL: max_q rows each.  Row i of n sees keys 0 .. kv_len - n + i (causal) or all kv_len of them,
  * of those without the skip_nearest last ones (the masked probe's o), of those the last `window` (0: all).  Query head h reads key head
  * h / (n_heads / n_kv_heads).  Scores are scaled by `scale`.  A row that sees no key, or none with a score above -inf, gets zeros.  Keys
- * on pages that the cache does not have are not seen.  A sequence's rows beyond max_q are left as they are, its keys beyond max_kv and
+ * on pages that the cache does not have are not seen.  Sums are held in float32, relative to a reference up to 2^8 below the largest
+ * probability: values over 2^96 can overflow them.  A sequence's rows beyond max_q are left as they are, its keys beyond max_kv and
  * max_pages pages do not count; rows of no sequence are left as they are.
  * Long sequences are cut in pieces that are joined in order in a second launch; how they are cut depends on the struct's numbers alone, and
  * the same call gives the same bits.  The pieces need a workspace (see below) that is the call's own until its work has ended. */
@@ -325,7 +327,7 @@ typedef struct {
     const int32_t *q_start_dev;   /* [n_seqs + 1], nullable */
     const int32_t *kv_len_dev;    /* [n_seqs] */
     const int32_t *page_table_dev;
-    int32_t n_seqs, n_heads, n_rows;
+    int32_t n_seqs, n_heads, n_rows; /* n_seqs <= 65535, n_seqs * n_heads * max_q and max_q * (n_heads / n_kv_heads)^2 < 2^31 */
     int32_t max_pages;            /* entries of a sequence's row of the table */
     int32_t max_q, max_kv;        /* bounds of what q_start_dev and kv_len_dev hold */
     int32_t causal, skip_nearest, window;

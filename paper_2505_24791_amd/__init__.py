@@ -425,8 +425,12 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
     lens = _ints(kv_len, "kv_len", (seqs,), device)
     start = _ints(q_start, "q_start", (seqs + 1,), device) if q_start is not None else None
     out, out_stride = _into(out, q, shape, cache.dtype, "out", device)
+    if max_kv is None:
+        max_kv = pages * KV4_PAGE
+    if not 0 <= max_q | max_kv | skip_nearest | window < 2 ** 31:
+        _refuse("max_q, max_kv, skip_nearest and window are non-negative 32-bit integers")
     a = SjdKv4Attention(q.data_ptr(), out.data_ptr(), q_stride, out_stride, table_stride[0], start, lens, page_table.data_ptr(),
-                        seqs, heads, n, pages, max_q, pages * KV4_PAGE if max_kv is None else max_kv, 1 if causal else 0, skip_nearest,
+                        seqs, heads, n, pages, max_q, max_kv, 1 if causal else 0, skip_nearest,
                         window, dim ** -0.5 if scale is None else scale, None, 0)
     lib = _rt[0]
     address, need = C.addressof(a), C.c_size_t()

@@ -56,24 +56,24 @@ template <typename F> __device__ __forceinline__ float over_row(float v, F f) {
 __device__ __forceinline__ float row_max(float v) { return over_row(v, [](float x, float y) { return fmaxf(x, y); }); }
 __device__ __forceinline__ float row_sum(float v) { return over_row(v, [](float x, float y) { return x + y; }); }
 
-struct Seq { int row0, n, len; };      // first row, rows and keys of a sequence, within what the call allows
+struct Seq { int row0, n, len, all; };      // first row, rows and keys of a sequence, within what the call allows; rows that it would have
 __device__ __forceinline__ Seq sequence(const Kv4Attn &a, int b) {
     Seq s;
     if (a.q_start) {
         s.row0 = min(max(a.q_start[b], 0), a.n_rows);
-        s.n = min(min(max(a.q_start[b + 1], s.row0), a.n_rows) - s.row0, a.max_q);
+        s.all = min(max(a.q_start[b + 1], s.row0), a.n_rows) - s.row0;
+        s.n = min(s.all, a.max_q);
     } else {
         s.row0 = b * a.max_q;
-        s.n = a.max_q;
+        s.n = s.all = a.max_q;
     }
     s.len = min(min(max(a.kv_len[b], 0), a.max_kv), a.max_pages * kKv4Page);
     return s;
 }
 // keys first .. last of the i-th new token of a sequence (none: last < first)
 __device__ __forceinline__ void seen(const Kv4Attn &a, const Seq &s, int i, int &first, int &last) {
-    last = (a.causal ? s.len - s.n + i : s.len - 1) - a.skip;
+    last = max((a.causal ? s.len - s.all + i : s.len - 1) - a.skip, -1);
     first = a.window ? max(0, last - a.window + 1) : 0;
-    last = max(last, -1);
 }
 
 // ------------------------------------------------------------------------------------------------

@@ -1570,7 +1570,7 @@ int check_attention(const sjd_kv4 *c, const sjd_kv4_attention *g, Kv4Attn *out) 
     if ((rc = check_heads(g->n_heads, c->n_kv_heads))) return rc;
     if (g->n_seqs < 0 || g->n_rows < 0 || g->max_pages < 0 || g->max_q < 0 || g->max_kv < 0) return fail(SJD_EINVAL, "a count is negative");
     if (g->skip_nearest < 0 || g->window < 0) return fail(SJD_EINVAL, "skip_nearest and window must not be negative");
-    if (!(g->scale > 0.f && isfinite(g->scale))) return fail(SJD_EINVAL, "scale must be finite and above 0");
+    if (!(g->scale > 0.f && isfinite(2.f * g->scale))) return fail(SJD_EINVAL, "scale must be above 0 and below 2^127");
     if (!g->q_start_dev && (int64_t)g->n_seqs * g->max_q != g->n_rows) return fail(SJD_EINVAL, "without q_start_dev there are n_seqs * max_q rows");
     if ((int64_t)g->max_q * g->n_heads > INT32_MAX / 2 || g->max_kv > INT32_MAX / 2 || g->max_pages > INT32_MAX / SJD_KV4_PAGE ||
         (int64_t)g->n_seqs * g->max_q > (int64_t)1 << 40)
@@ -1580,7 +1580,9 @@ int check_attention(const sjd_kv4 *c, const sjd_kv4_attention *g, Kv4Attn *out) 
     a.n_seqs = g->n_seqs; a.n_heads = g->n_heads; a.n_rows = g->n_rows; a.max_pages = g->max_pages;
     a.max_q = g->max_q < g->n_rows ? g->max_q : g->n_rows;      // no sequence has more rows than there are
     a.max_kv = (int)((int64_t)g->max_pages * SJD_KV4_PAGE < g->max_kv ? (int64_t)g->max_pages * SJD_KV4_PAGE : g->max_kv);
-    a.causal = g->causal != 0; a.skip = g->skip_nearest; a.window = g->window;
+    a.causal = g->causal != 0;
+    a.skip = g->skip_nearest < a.max_kv ? g->skip_nearest : a.max_kv;      // so many leave nothing; nothing overflows
+    a.window = g->window < a.max_kv ? g->window : 0;
     a.scale_log2 = g->scale * 1.44269504088896340736f;
     if (!kv4_attention_plan(a, c->dtype == SJD_DTYPE_F32)) return fail(SJD_EINVAL, "too many rows or sequences for one call");
     *out = a;

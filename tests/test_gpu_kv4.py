@@ -372,6 +372,30 @@ def test_scale_and_scores_that_differ_by_much(torch_cuda):
     _check(torch, got, q, [0, 1], [500], keys, values, "float32", scale=2.5)
 
 
+def test_bounds_that_are_too_small_and_distances_to_the_ends_of_int32(torch_cuda):
+    """Rows beyond max_q stay, the ones before see what they see otherwise; a window or a distance of 2^31 - 1, more new rows than keys."""
+    import paper_2505_24791_amd as sjd
+    torch = torch_cuda
+    rng = np.random.default_rng(31)
+    cache, table, kv_len, keys, values = _filled(torch, sjd, rng, "float16", 2, 64, [300, 5])
+    start, top = [0, 40, 70], 2 ** 31 - 1
+    q = _rows(torch, rng, 70, 4, 64, "float16")
+    kw = dict(q_start=torch.tensor(start, dtype=torch.int32, device="cuda"), max_kv=300)
+    full = sjd.op_kv4_attention(cache, q, table, kv_len, max_q=40, **kw)
+    _check(torch, full, q, start, [300, 5], keys, values, "float16")
+    assert not full[40:65].any()                                           # 30 new tokens of which 5 are cached: the first 25 see nothing
+    few = sjd.op_kv4_attention(cache, q, table, kv_len, max_q=33, out=torch.full_like(q, 7.0), **kw)
+    assert bool((few[33:40] == 7).all())
+    _check(torch, torch.cat([few[:33], full[33:40], few[40:]]), q, start, [300, 5], keys, values, "float16")
+    wide = sjd.op_kv4_attention(cache, q, table, kv_len, max_q=40, window=top, **kw)
+    assert torch.equal(wide, full)
+    for skip, window in ((top, 0), (top, top), (301, 1)):
+        assert not sjd.op_kv4_attention(cache, q, table, kv_len, max_q=40, skip_nearest=skip, window=window, **kw).any()
+    for bad in (dict(window=2 ** 32), dict(skip_nearest=2 ** 32 + 1), dict(max_q=2 ** 32 + 40), dict(max_kv=2 ** 32 + 300)):
+        with pytest.raises(sjd.SjdError):
+            sjd.op_kv4_attention(cache, q, table, kv_len, **{**dict(max_q=40), **kw, **bad})
+
+
 def test_pages_that_the_cache_does_not_have_are_not_seen(torch_cuda):
     import paper_2505_24791_amd as sjd
     torch = torch_cuda

@@ -110,6 +110,16 @@ def test_attention_that_is_refused(lib, kw, word):
     assert word in lib.sjd_last_error().decode()
 
 
+@pytest.mark.parametrize("kw,word", [
+    (dict(scale=3e38), "scale"), (dict(scale=float("nan")), "scale"), (dict(scale=float("inf")), "scale"), (dict(n_seqs=65536, n_rows=65536), "too many"),
+    (dict(n_heads=64, max_q=2 ** 21, n_rows=3 * 2 ** 21), "too many")])
+def test_attention_beyond_its_ranges_is_refused(lib, kw, word):
+    a, c, n = _attn(**kw), _cache(), C.c_size_t()
+    for call in (lambda: lib.sjd_op_kv4_attention(C.addressof(c), C.addressof(a), None),
+                 lambda: lib.sjd_kv4_attention_workspace(C.addressof(c), C.addressof(a), C.addressof(n))):
+        assert call() == sjd.SJD_EINVAL and word in lib.sjd_last_error().decode()
+
+
 def test_attention_asks_for_its_workspace(lib):
     c, need = _cache(), C.c_size_t(0)
     a = _attn(max_pages=4000, max_kv=250000)
