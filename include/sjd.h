@@ -259,7 +259,8 @@ SJD_API int sjd_op_attention_h16(int dtype, const void *qkv_dev, void *o_dev, in
  * column, time) and hold their key/value cache in 4 bits.  They only enqueue work on `hip_stream`: no call here waits, allocates, or keeps
  * anything, so each can be captured into a graph.  All pointers are DEVICE memory of the current device, rows of `dtype`
  * (SJD_DTYPE_*) whose heads follow one another, rows `*_stride` ELEMENTS apart; nothing has to start on more than a
- * multiple of its own element.  No rows (n_rows = 0) is a call that does nothing. */
+ * multiple of its own element.  No rows (n_rows = 0) is a call that does nothing.  Rows times heads (of queries and keys
+ * together) times head_dim, rounded up to 32, 64, 128 or 256, stay below 2^34. */
 
 /* Norms and rotation, in this order.  A norm runs over the head_dim channels of one head of one row:
  *   norm 0: none;   1: x / sqrt(mean x^2 + eps) * gain (+ shift);   2: (x - mean x) / sqrt(var x + eps) * gain + shift
@@ -301,7 +302,7 @@ typedef struct {
 /* Keys and values of n_rows tokens into the cache: row i becomes token slot_dev[i] % 64 of page slot_dev[i] / 64 (int32; a slot outside the
  * cache, such as -1, is left out; a slot given twice holds a mixture of its rows).  opts NULL: as they are.  Otherwise the keys are normed and
  * rotated first (rounded to dtype, as sjd_op_qk_norm_rope gives them: the cache gets the same bits), and with q_dev (nullable)
- * the queries of the same rows go to q_out_dev in the same launch; n_kv_heads * head_dim <= 8192 then. */
+ * the queries of the same rows go to q_out_dev (which may be q_dev) in the same launch; n_kv_heads * head_dim <= 8192 then. */
 SJD_API int sjd_op_kv4_write(const sjd_kv4 *cache, const int32_t *slot_dev, const void *k_dev, int64_t k_stride, const void *v_dev,
                              int64_t v_stride, int n_rows, const sjd_qk_opts *opts, const int32_t *pos_dev, const void *q_dev,
                              int64_t q_stride, int n_heads, void *q_out_dev, int64_t q_out_stride, void *hip_stream);

@@ -1555,10 +1555,11 @@ int check_heads(int n_heads, int n_kv) {
     return SJD_OK;
 }
 
-// grids are counted in 31 bits
-int check_work(int64_t n_rows, int64_t heads, int64_t chunks) {
+// Grids are counted in 32 bits of threads: 4 to 32 (a power of two of at least dim / 8) for a head of a row, at most twice as many where LDS holds few rows.
+int check_work(int64_t n_rows, int64_t heads, int dim) {
+    const int64_t lanes = dim <= 32 ? 4 : dim <= 64 ? 8 : dim <= 128 ? 16 : 32;
     if (n_rows < 0) return fail(SJD_EINVAL, "n_rows must not be negative");
-    if (n_rows * heads > (int64_t)INT32_MAX * 8 || n_rows * heads / 256 * chunks + 2 > INT32_MAX) return fail(SJD_EINVAL, "too many rows for one call");
+    if (n_rows * heads * lanes > INT32_MAX) return fail(SJD_EINVAL, "too many rows for one call");
     return SJD_OK;
 }
 
@@ -1604,7 +1605,7 @@ int sjd_op_qk_norm_rope(int dtype, const sjd_qk_opts *opts, const int32_t *pos_d
     const int hq = q_dev ? n_heads : 0, hk = k_dev ? n_kv_heads : 0;
     QkOpts o;
     int rc;
-    if ((rc = check_work(n_rows, hq + hk, 1)) || (rc = check_qk_opts(opts, pos_dev, head_dim, &o))) return rc;
+    if ((rc = check_work(n_rows, hq + hk, head_dim)) || (rc = check_qk_opts(opts, pos_dev, head_dim, &o))) return rc;
     if (q_dev && ((rc = check_rows("q_dev", dtype, q_dev, q_stride, (int64_t)hq * head_dim, n_rows, false)) ||
                   (rc = check_rows("q_out_dev", dtype, q_out_dev, q_out_stride, (int64_t)hq * head_dim, n_rows, true)))) return rc;
     if (k_dev && ((rc = check_rows("k_dev", dtype, k_dev, k_stride, (int64_t)hk * head_dim, n_rows, false)) ||
@@ -1623,7 +1624,7 @@ int sjd_op_kv4_write(const sjd_kv4 *cache, const int32_t *slot_dev, const void *
                      int64_t q_stride, int n_heads, void *q_out_dev, int64_t q_out_stride, void *hip_stream) {
     Kv4Cache c;
     int rc = check_cache(cache, &c);
-    if (rc || (rc = check_work(n_rows, (int64_t)c.n_heads + (q_dev ? n_heads : 0), 32))) return rc;
+    if (rc || (rc = check_work(n_rows, (int64_t)c.n_heads + (q_dev ? n_heads : 0), c.dim))) return rc;
     const int64_t width = (int64_t)c.n_heads * c.dim;
     QkOpts o;
     if (opts) {
@@ -1654,7 +1655,7 @@ int sjd_op_kv4_read(const sjd_kv4 *cache, const int32_t *slot_dev, void *k_dev, 
                     int n_rows, void *hip_stream) {
     Kv4Cache c;
     int rc = check_cache(cache, &c);
-    if (rc || (rc = check_work(n_rows, c.n_heads, 32))) return rc;
+    if (rc || (rc = check_work(n_rows, c.n_heads, c.dim))) return rc;
     if (n_rows == 0) return SJD_OK;
     const int64_t width = (int64_t)c.n_heads * c.dim;
     if ((rc = check_pages(cache))) return rc;

@@ -46,6 +46,16 @@ def test_norm_and_rotation_refuses(lib, o, kw, word):
     assert word in lib.sjd_last_error().decode()
 
 
+@pytest.mark.parametrize("dim,rows", [(32, 2 ** 27), (64, 2 ** 26), (128, 2 ** 25), (256, 2 ** 24)])
+def test_more_rows_than_a_launch_counts_are_refused(lib, dim, rows):
+    c, w = _cache(head_dim=dim, n_kv_heads=4), 4 * dim
+    calls = (lambda: lib.sjd_op_kv4_write(C.addressof(c), PTR, PTR, w, PTR, w, rows, None, None, None, 0, 0, None, 0, None),
+             lambda: lib.sjd_op_kv4_read(C.addressof(c), PTR, PTR, w, PTR, w, rows, None),
+             lambda: _rope(lib, _opts(norm=0, rot_dim=0, freq=None), heads=2, kv=2, dim=dim, qs=w, ks=w, qos=w, kos=w, n=rows))
+    for call in calls:
+        assert call() == sjd.SJD_EINVAL and "too many" in lib.sjd_last_error().decode()
+
+
 def test_nothing_to_do_is_no_error(lib):
     assert _rope(lib, _opts(), n=0, q=None, k=None, qo=None, ko=None) == sjd.SJD_OK
     c = _cache(pages=None)
