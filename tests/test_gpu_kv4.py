@@ -182,6 +182,36 @@ def test_written_tokens_read_back_as_the_format_says(torch_cuda, name, dim, kv, 
     assert not z[0].any() and not z[1].any()
 
 
+@pytest.mark.parametrize("dim", [32, 64, 128, 256])
+@pytest.mark.parametrize("order", ["on", "shifted", "holes", "swapped", "backward", "ends"])
+def test_tokens_in_and_out_of_order(torch_cuda, dim, order):
+    """Runs of tokens from page starts and from elsewhere, with rows left out in between, pairs swapped, backward, and slots around the ends of the cache."""
+    import paper_2505_24791_amd as sjd
+    torch = torch_cuda
+    rng = np.random.default_rng(dim)
+    n, kv = 193, 2
+    k, v = (torch.from_numpy(_special(rng, n, kv, dim, "bfloat16")).to(torch.bfloat16).cuda() for _ in range(2))
+    t = np.arange(n)
+    slots = {"on": t, "shifted": t + 3, "holes": np.where(t % 5 == 2, -1, t), "swapped": t ^ 1, "backward": n + 2 - t, "ends": t - 2}[order].astype(np.int64)
+    pages = 4
+    if order == "ends":
+        slots = np.where(t >= 100, slots + pages * 64 - 150, slots)               # 98 .. before the end and past it
+        slots[[7, 8, 9, 10, 11, 12]] = [-2 ** 31, 2 ** 31 - 1, -2 ** 31, -2 ** 31 + 1, -2 ** 31 + 2, -2 ** 31 + 3]
+    cache = sjd.Kv4Cache(torch.full((pages, kv, 68 * dim), 0x5A, dtype=torch.uint8, device="cuda"), torch.bfloat16)
+    everything = torch.arange(pages * 64, dtype=torch.int32, device="cuda")
+    before = [_f64(x) for x in sjd.op_kv4_read(cache, everything)]
+    slot = torch.from_numpy(slots.astype(np.int32)).cuda()
+    sjd.op_kv4_write(cache, k, v, slot)
+    fused = sjd.Kv4Cache(torch.full_like(cache.pages, 0x5A), torch.bfloat16)
+    sjd.op_kv4_write(fused, k, v, slot, opts=sjd.QkOpts(norm="none"))
+    inside = (slots >= 0) & (slots < pages * 64)
+    assert len(set(slots[inside])) == inside.sum() > 90
+    for got, x, old in zip(sjd.op_kv4_read(cache, everything), (k, v), before):
+        old[slots[inside]] = held(_f64(x), "bfloat16")[inside]
+        assert np.array_equal(_f64(got), old)
+    assert torch.equal(fused.pages, cache.pages)
+
+
 @pytest.mark.parametrize("name", TYPES)
 def test_groups_with_nan_or_infinity_read_as_nan(torch_cuda, name):
     import paper_2505_24791_amd as sjd
