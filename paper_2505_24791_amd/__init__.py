@@ -327,6 +327,8 @@ def op_qk_norm_rope(q, k, pos, opts: QkOpts, *, q_out=None, k_out=None):
     if some is None:
         _refuse("need q or k")
     dtype, device = some.dtype, some.get_device()
+    if device < 0:         # host memory: options without vectors, and the other tensors of the call, would agree with it
+        _refuse("need rows on the GPU")
     code = _row_dtype(dtype)
     qp = qs = qh = qo = qos = kp = ks = kh = ko = kos = 0
     if q is not None:
