@@ -280,7 +280,8 @@ def _launch(device: int, fn, *args) -> None:
 
 
 class QkOpts:
-    """Norms and rotation of queries and keys (``sjd_qk_opts``), made once and used by many calls; it holds on to its tensors.
+    """Norms and rotation of queries and keys (``sjd_qk_opts``), made once and used by many calls; it holds on to its tensors, and a call reads
+    them where they are then (a captured graph where they were when it was captured).
 
     ``norm``: "none", "rms" or "layer" over the channels of a head, with gains and shifts [head_dim] float32 or None.  ``axis_pairs``: how
     many channel pairs each axis of the positions turns, together ``rot_dim / 2``; ``freq`` [rot_dim / 2] float32: radians per step of
@@ -288,32 +289,47 @@ class QkOpts:
 
     def __init__(self, *, norm: Optional[str] = "rms", eps: float = 1e-6, q_gain=None, q_shift=None, k_gain=None, k_shift=None,
                  rot_dim: int = 0, adjacent: bool = False, axis_pairs: Tuple[int, ...] = (), freq=None):
-        import torch
         if norm not in _NORMS:
             _refuse(f"norm must be one of {[n for n in _NORMS if n]}")
         if rot_dim and (not 1 <= len(axis_pairs) <= 4 or freq is None):
             _refuse("a rotation needs axis_pairs of 1 to 4 axes and freq")
         vectors = {"q_gain": q_gain, "q_shift": q_shift, "k_gain": k_gain, "k_shift": k_shift, "freq": freq}
-        self.tensors = [t for t in vectors.values() if t is not None]
-        for name, t in vectors.items():
-            if t is not None and not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 1):
+        self.vectors = {name: t for name, t in vectors.items() if t is not None}
+        self.n_axes = len(axis_pairs) if rot_dim else 0
+        self.c = SjdQkOpts(_NORMS[norm], eps, None, None, None, None, rot_dim, 1 if adjacent else 0, self.n_axes,
+                           (C.c_int32 * 4)(*axis_pairs[:4]), None)
+        self.address = C.addressof(self.c)
+        self._take()
+
+    def _take(self) -> None:
+        """Checks the vectors and puts their addresses into the struct."""
+        import torch
+        held = []
+        for name, t in self.vectors.items():
+            if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 1):
                 _refuse(f"{name}: need a contiguous float32 vector on the GPU")
-        if freq is not None and freq.numel() != rot_dim // 2:
+            held.append((t, t.data_ptr()))
+            if t.numel() and not held[-1][1]:
+                _refuse(f"{name}: its memory has been freed")
+        freq = self.vectors.get("freq")
+        if freq is not None and freq.numel() != self.c.rot_dim // 2:
             _refuse("freq: need rot_dim / 2 values")
-        sizes = {t.numel() for name, t in vectors.items() if t is not None and name != "freq"}
-        devices = {t.get_device() for t in self.tensors}
+        sizes = {t.numel() for name, t in self.vectors.items() if name != "freq"}
+        devices = {t.get_device() for t in self.vectors.values()}
         if len(sizes) > 1 or len(devices) > 1:
             _refuse("gains and shifts need one size, and all vectors one device")
         self.head_dim = sizes.pop() if sizes else None      # None: any
         self.device = devices.pop() if devices else None
-        self.n_axes = len(axis_pairs) if rot_dim else 0
-        ptr = lambda t: t.data_ptr() if t is not None else None
-        self.c = SjdQkOpts(_NORMS[norm], eps, ptr(q_gain), ptr(q_shift), ptr(k_gain), ptr(k_shift), rot_dim, 1 if adjacent else 0,
-                           self.n_axes, (C.c_int32 * 4)(*axis_pairs[:4]), ptr(freq))
-        self.address = C.addressof(self.c)
+        for name, (_, at) in zip(self.vectors, held):
+            setattr(self.c, name, at)
+        self._held = held
 
     def _for(self, head_dim: int, device: int) -> int:
         """The struct's address, for rows of this head size on this device."""
+        for t, at in self._held:
+            if t.data_ptr() != at:                          # its storage was replaced: the old one may be anyone's by now
+                self._take()
+                break
         if (self.head_dim is not None and self.head_dim != head_dim) or (self.device is not None and self.device != device):
             _refuse(f"the options hold vectors of {self.head_dim} values on cuda:{self.device}, the rows are of {head_dim} on cuda:{device}")
         return self.address
@@ -350,16 +366,30 @@ def op_qk_norm_rope(q, k, pos, opts: QkOpts, *, q_out=None, k_out=None):
 
 class Kv4Cache:
     """A key/value cache of one layer in 4 bits (``sjd_kv4``): ``pages`` uint8 [pages, kv_heads, 68 * head_dim], 64 tokens to a page, of rows
-    of ``dtype``.  The pages are the caller's: any tensor of that shape, e.g. ``Kv4Cache.zeros(...)``."""
+    of ``dtype``.  The pages are the caller's: any tensor of that shape, e.g. ``Kv4Cache.zeros(...)``.  A call takes ``pages`` as it is then."""
 
     def __init__(self, pages, dtype):
+        self.pages, self.dtype = pages, dtype
+        self.c = SjdKv4(None, 0, 0, 0, _row_dtype(dtype))
+        self.address = C.addressof(self.c)
+        self._take()
+
+    def _take(self) -> None:
         import torch
+        pages = self.pages
         if not (pages.is_cuda and pages.dtype == torch.uint8 and pages.is_contiguous() and pages.dim() == 3 and pages.shape[2] % 68 == 0):
             _refuse("pages: need a contiguous uint8 tensor [pages, kv_heads, 68 * head_dim] on the GPU")
-        self.pages, self.dtype, self.device = pages, dtype, pages.get_device()
+        self.device = pages.get_device()
         self.n_pages, self.kv_heads, self.head_dim = pages.shape[0], pages.shape[1], pages.shape[2] // 68
-        self.c = SjdKv4(pages.data_ptr(), self.n_pages, self.kv_heads, self.head_dim, _row_dtype(dtype))
-        self.address = C.addressof(self.c)
+        c = self.c
+        self._from, self._at = pages, pages.data_ptr()
+        c.pages, c.n_pages, c.n_kv_heads, c.head_dim = self._at, self.n_pages, self.kv_heads, self.head_dim
+
+    def _now(self) -> int:
+        """The struct's address, for the pages as they are."""
+        if self.pages is not self._from or self._from.data_ptr() != self._at:      # replaced: the old memory may be anyone's by now
+            self._take()
+        return self.address
 
     @classmethod
     def zeros(cls, n_pages: int, kv_heads: int, head_dim: int, dtype, device="cuda"):
@@ -377,6 +407,7 @@ def op_kv4_write(cache: Kv4Cache, k, v, slot, *, opts: Optional[QkOpts] = None, 
     """``sjd_op_kv4_write``: rows k, v [rows, kv_heads, head_dim] become the tokens ``slot`` [rows] int32 (page * 64 + offset; -1: left out).
     With ``opts`` the keys are normed and rotated first, and with ``q`` [rows, heads, head_dim] the queries of those rows too: returns them
     (``q_out`` or a new tensor), else None."""
+    to = cache._now()
     n, device, dim = k.shape[0], cache.device, cache.head_dim
     (kp, ks), (vp_, vs) = cache._kv(k, "k", n), cache._kv(v, "v", n)
     sp = _ints(slot, "slot", (n,), device)
@@ -394,18 +425,18 @@ def op_kv4_write(cache: Kv4Cache, k, v, slot, *, opts: Optional[QkOpts] = None, 
             _refuse("q: other rows or another head size")
         q_out, qos = _into(q_out, q, shape, cache.dtype, "q_out", device)
         qp, heads, qo = q.data_ptr(), shape[1], q_out.data_ptr()
-    _launch(device, _rt[0].sjd_op_kv4_write, cache.address, sp, kp, ks, vp_, vs, n, op, pp, qp, qs, heads, qo, qos)
+    _launch(device, _rt[0].sjd_op_kv4_write, to, sp, kp, ks, vp_, vs, n, op, pp, qp, qs, heads, qo, qos)
     return q_out if q is not None else None
 
 
 def op_kv4_read(cache: Kv4Cache, slot, *, k_out=None, v_out=None):
     """``sjd_op_kv4_read``: the tokens ``slot`` [rows] int32 of the cache, (k, v) [rows, kv_heads, head_dim]; zeros for a slot outside it."""
-    n, device = slot.shape[0], cache.device
+    held, n, device = cache._now(), slot.shape[0], cache.device
     sp = _ints(slot, "slot", (n,), device)
     shape = (n, cache.kv_heads, cache.head_dim)
     k_out, ks = _into(k_out, cache.pages, shape, cache.dtype, "k_out", device)
     v_out, vs = _into(v_out, cache.pages, shape, cache.dtype, "v_out", device)
-    _launch(device, _rt[0].sjd_op_kv4_read, cache.address, sp, k_out.data_ptr(), ks, v_out.data_ptr(), vs, n)
+    _launch(device, _rt[0].sjd_op_kv4_read, held, sp, k_out.data_ptr(), ks, v_out.data_ptr(), vs, n)
     return k_out, v_out
 
 
@@ -415,7 +446,7 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
     page_table [seqs, max_pages] int32; sequence b has the rows q_start[b] .. q_start[b+1] - 1 (q_start [seqs + 1] int32; None: max_q
     each).  max_q and max_kv bound the rows and keys of a sequence (max_kv None: all that the table has room for).  Rows of no
     sequence are left as they are in ``out`` (None: a new tensor, which holds anything there)."""
-    device = cache.device
+    held, device = cache._now(), cache.device
     shape, q_stride = _rows3(q, "q", cache.dtype, device)
     n, heads, dim = shape
     if dim != cache.head_dim:
@@ -436,13 +467,13 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
                         window, dim ** -0.5 if scale is None else scale, None, 0)
     lib = _rt[0]
     address, need = C.addressof(a), C.c_size_t()
-    rc = lib.sjd_kv4_attention_workspace(cache.address, address, C.addressof(need))
+    rc = lib.sjd_kv4_attention_workspace(held, address, C.addressof(need))
     if rc:
         _check(rc)
     if need.value:
         workspace = cache.pages.new_empty(need.value)
         a.workspace, a.workspace_bytes = workspace.data_ptr(), need.value
-    _launch(device, lib.sjd_op_kv4_attention, cache.address, address)
+    _launch(device, lib.sjd_op_kv4_attention, held, address)
     return out
 
 
