@@ -215,6 +215,7 @@ def op_attention_h16(qkv, n_samples, T, H):
 
 
 KV4_PAGE = 64          # tokens of a page of the 4-bit cache
+_MOST = 2 ** 31 - 1    # the library counts in 32 bits, and ctypes drops the others without a word
 _NORMS = {None: 0, "none": 0, "rms": 1, "layer": 2}
 _rt = None             # what the calls below use of the library and of torch, once both are loaded
 
@@ -248,6 +249,8 @@ def _rows3(t, what: str, dtype, device: int):
         _refuse(f"{what}: need a {dtype} tensor [rows, heads, head_dim] on cuda:{device}")
     if ((stride[1] != shape[2] and shape[1] != 1) or (stride[2] != 1 and shape[2] != 1)) and shape[0]:
         _refuse(f"{what}: the heads of a row must follow one another")
+    if shape[0] | shape[1] | shape[2] > _MOST:
+        _refuse(f"{what}: too many rows for one call")
     return shape, stride[0]
 
 
@@ -293,6 +296,8 @@ class QkOpts:
             _refuse(f"norm must be one of {[n for n in _NORMS if n]}")
         if rot_dim and (not 1 <= len(axis_pairs) <= 4 or freq is None):
             _refuse("a rotation needs axis_pairs of 1 to 4 axes and freq")
+        if rot_dim and (min(axis_pairs) < 0 or sum(axis_pairs) != rot_dim // 2):
+            _refuse("axis_pairs must not be negative and add up to rot_dim / 2")
         vectors = {"q_gain": q_gain, "q_shift": q_shift, "k_gain": k_gain, "k_shift": k_shift, "freq": freq}
         self.vectors = {name: t for name, t in vectors.items() if t is not None}
         self.n_axes = len(axis_pairs) if rot_dim else 0
@@ -433,6 +438,8 @@ def op_kv4_read(cache: Kv4Cache, slot, *, k_out=None, v_out=None):
     """``sjd_op_kv4_read``: the tokens ``slot`` [rows] int32 of the cache, (k, v) [rows, kv_heads, head_dim]; zeros for a slot outside it."""
     held, n, device = cache._now(), slot.shape[0], cache.device
     sp = _ints(slot, "slot", (n,), device)
+    if n > _MOST:
+        _refuse("slot: too many rows for one call")
     shape = (n, cache.kv_heads, cache.head_dim)
     k_out, ks = _into(k_out, cache.pages, shape, cache.dtype, "k_out", device)
     v_out, vs = _into(v_out, cache.pages, shape, cache.dtype, "v_out", device)
@@ -455,12 +462,14 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
     if page_table.dtype is not _rt[4] or page_table.get_device() != device or len(table_shape) != 2 or (table_shape[1] > 1 and table_stride[1] != 1):
         _refuse(f"page_table: need int32 rows [seqs, max_pages] on cuda:{device}")
     seqs, pages = table_shape
+    if seqs | pages > _MOST:
+        _refuse("page_table: too many sequences or pages for one call")
     lens = _ints(kv_len, "kv_len", (seqs,), device)
     start = _ints(q_start, "q_start", (seqs + 1,), device) if q_start is not None else None
     out, out_stride = _into(out, q, shape, cache.dtype, "out", device)
     if max_kv is None:
         max_kv = pages * KV4_PAGE
-    if not 0 <= max_q | max_kv | skip_nearest | window < 2 ** 31:
+    if not 0 <= max_q | max_kv | skip_nearest | window <= _MOST:
         _refuse("max_q, max_kv, skip_nearest and window are non-negative 32-bit integers")
     a = SjdKv4Attention(q.data_ptr(), out.data_ptr(), q_stride, out_stride, table_stride[0], start, lens, page_table.data_ptr(),
                         seqs, heads, n, pages, max_q, max_kv, 1 if causal else 0, skip_nearest,

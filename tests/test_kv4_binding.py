@@ -125,3 +125,28 @@ def test_caches_follow_their_pages(stub):
         with pytest.raises(sjd.SjdError):
             call()
     assert len(stub.calls) == done
+
+
+MANY = 2 ** 32 + 4          # 4 to a call that counts in 32 bits
+
+
+def test_counts_beyond_32_bits_are_refused(stub):
+    """Rows that all lie in the same memory (``expand``) can be so many, and so can a page table's entries."""
+    i32 = lambda *s: Fake(s, torch.int32)
+    rows = lambda n, h, d: Fake((n, h, d), torch.float16, stride=(0 if n == MANY else h * d, d, 1))
+    cache = sjd.Kv4Cache(Fake((2, 2, 68 * 64), torch.uint8), torch.float16)
+    none, x = sjd.QkOpts(), rows(4, 2, 64)
+    for call in (lambda: sjd.op_qk_norm_rope(rows(MANY, 2, 64), None, None, none), lambda: sjd.op_qk_norm_rope(None, rows(MANY, 2, 64), None, none),
+                 lambda: sjd.op_qk_norm_rope(rows(4, MANY, 64), None, None, none), lambda: sjd.op_qk_norm_rope(rows(4, 1, MANY + 60), None, None, none),
+                 lambda: sjd.op_kv4_write(cache, rows(MANY, 2, 64), rows(MANY, 2, 64), i32(MANY)),
+                 lambda: sjd.op_kv4_write(cache, x, x, i32(4), q=rows(4, MANY, 64), opts=none),
+                 lambda: sjd.op_kv4_read(cache, i32(MANY)),
+                 lambda: sjd.op_kv4_attention(cache, rows(MANY, 2, 64), i32(MANY, 1), i32(MANY)),
+                 lambda: sjd.op_kv4_attention(cache, rows(4, MANY, 64), i32(4, 1), i32(4)),
+                 lambda: sjd.op_kv4_attention(cache, x, i32(MANY, 1), i32(MANY), q_start=i32(MANY + 1)),
+                 lambda: sjd.op_kv4_attention(cache, x, i32(4, MANY), i32(4), max_kv=100),
+                 lambda: sjd.QkOpts(rot_dim=64, axis_pairs=(2 ** 32 + 16, 16), freq=Fake((32,), torch.float32)),
+                 lambda: sjd.QkOpts(rot_dim=64, axis_pairs=(2 ** 32 + 16, 16 - 2 ** 32), freq=Fake((32,), torch.float32))):
+        with pytest.raises(sjd.SjdError):
+            call()
+    assert not stub.calls
