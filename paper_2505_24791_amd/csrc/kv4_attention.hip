@@ -88,6 +88,10 @@ __device__ __forceinline__ void seen(const Kv4Attn &a, const Seq &s, int i, int 
 // faster on such sequences.
 constexpr int kRows = 16;
 constexpr float kLag = 8.f;                       // base 2
+// The reference m of a row lies `over` below the maximum that it was taken from, so that the largest probability of a wave is 2^over to 2^(over + kLag).
+// Half: 2^15 still fits, and probabilities down to 2^-21 of the largest keep their 11 bits, those down to 2^-32 are there; with m at the maximum itself
+// a wave lost every key 17.4 nats below its leading one, however many they are.  The other types have the exponents of float32.
+template <typename HT> constexpr float kOver = __is_same(HT, f16) ? 7.f : 0.f;
 
 // the new token of a row (rows are the query heads of a key head, token by token)
 __device__ __forceinline__ int token_of(const Kv4Attn &a, int row) { return a.group_magic ? (int)__umulhi((uint32_t)row, a.group_magic) : row; }
@@ -210,7 +214,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
         }
     }
     f32x4v o[NT][NG][2];
-    float m[NT], l[NT];                           // of the row (m scaled, base 2); of the lane's tokens of the row
+    float m[NT], l[NT];                           // of the row (the reference, scaled, base 2); of the lane's tokens of the row
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -257,10 +261,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
                     mx = fmaxf(mx, sc[n][t][e]);
                 }
             // The running maximum is only a reference: it moves when a score of some row is more than 2^kLag times over it, so that pages seldom
-            // exchange anything between lanes or touch the sums.  Probabilities then reach 2^kLag, which every operand type holds as exactly as 1.
+            // exchange anything between lanes or touch the sums.
             mx *= a.scale_log2;
-            if (__builtin_amdgcn_ballot_w64(!(mx <= m[n] + kLag)) != 0) {
-                const float m_new = fmaxf(m[n], row_max(mx));
+            if (__builtin_amdgcn_ballot_w64(!(mx <= m[n] + (kLag + kOver<HT>))) != 0) {
+                const float m_new = fmaxf(m[n], row_max(mx) - kOver<HT>);
                 const float corr = __builtin_amdgcn_exp2f(m[n] - (m_new == -INFINITY ? 0.f : m_new));
                 l[n] *= corr;
 #pragma unroll
