@@ -281,7 +281,7 @@ typedef struct {
 } sjd_qk_opts;
 
 /* q_out_dev = rotate(norm(q_dev)), and the same for keys; q_dev or k_dev may be NULL (that side is left out).  head_dim a multiple
- * of 8 up to 256.  pos_dev [n_rows, n_axes] int32.  An output may be its input (same pointer, same stride), else they must not overlap. */
+ * of 8 up to 256, n_heads and n_kv_heads up to 65535.  pos_dev [n_rows, n_axes] int32.  An output may be its input (same pointer, same stride), else they must not overlap. */
 SJD_API int sjd_op_qk_norm_rope(int dtype, const sjd_qk_opts *opts, const int32_t *pos_dev, const void *q_dev, int64_t q_stride,
                                 int n_heads, const void *k_dev, int64_t k_stride, int n_kv_heads, int head_dim, void *q_out_dev,
                                 int64_t q_out_stride, void *k_out_dev, int64_t k_out_stride, int n_rows, void *hip_stream);
@@ -291,7 +291,7 @@ SJD_API int sjd_op_qk_norm_rope(int dtype, const sjd_qk_opts *opts, const int32_
  * 2, 3, 4 or 6 times s, with its sign (nearest, ties to the even code; over 6 s: 6 s).  s lies in 2^-23 .. 2^13 for IEEE half rows,
  * else in 2^-125 .. 2^125; what is held has the type's values exactly.  A group with a NaN or an infinity reads as NaN.
  * Rows are read in the type they were written in.  The order inside a page is the library's.
- * head_dim 32, 64, 128 or 256. */
+ * head_dim 32, 64, 128 or 256; n_pages < 2^25, n_kv_heads <= 65535. */
 typedef struct {
     void *pages_dev;
     int32_t n_pages, n_kv_heads, head_dim;
@@ -302,7 +302,8 @@ typedef struct {
 /* Keys and values of n_rows tokens into the cache: row i becomes token slot_dev[i] % 64 of page slot_dev[i] / 64 (int32; a slot outside the
  * cache, such as -1, is left out; a slot given twice holds a mixture of its rows).  opts NULL: as they are.  Otherwise the keys are normed and
  * rotated first (rounded to dtype, as sjd_op_qk_norm_rope gives them: the cache gets the same bits), and with q_dev (nullable)
- * the queries of the same rows go to q_out_dev (which may be q_dev) in the same launch; n_kv_heads * head_dim <= 8192 then. */
+ * the queries of the same rows go to q_out_dev (which may be q_dev) in the same launch; n_kv_heads * head_dim <= 8192 then, and n_heads
+ * (<= 65535) a multiple of n_kv_heads. */
 SJD_API int sjd_op_kv4_write(const sjd_kv4 *cache, const int32_t *slot_dev, const void *k_dev, int64_t k_stride, const void *v_dev,
                              int64_t v_stride, int n_rows, const sjd_qk_opts *opts, const int32_t *pos_dev, const void *q_dev,
                              int64_t q_stride, int n_heads, void *q_out_dev, int64_t q_out_stride, void *hip_stream);
@@ -329,9 +330,10 @@ typedef struct {
     const int32_t *q_start_dev;   /* [n_seqs + 1], nullable */
     const int32_t *kv_len_dev;    /* [n_seqs] */
     const int32_t *page_table_dev;
-    int32_t n_seqs, n_heads, n_rows; /* n_seqs <= 65535, n_seqs * n_heads * max_q and max_q * (n_heads / n_kv_heads)^2 < 2^31 */
-    int32_t max_pages;            /* entries of a sequence's row of the table */
-    int32_t max_q, max_kv;        /* bounds of what q_start_dev and kv_len_dev hold */
+    int32_t n_seqs, n_heads, n_rows; /* n_seqs <= 65535, n_heads <= 65535 and a multiple of n_kv_heads */
+    int32_t max_pages;            /* entries of a sequence's row of the table; < 2^25 */
+    int32_t max_q, max_kv;        /* bounds of what q_start_dev and kv_len_dev hold; with no max_q beyond n_rows counted, n_seqs * n_heads * max_q and
+                                     max_q * (n_heads / n_kv_heads)^2 < 2^31, max_q * n_heads < 2^30; max_kv < 2^30 */
     int32_t causal, skip_nearest, window;
     float scale;                  /* > 0 */
     void *workspace_dev;          /* 16-byte boundary; may be NULL where none is needed */

@@ -72,12 +72,13 @@ struct Kv4Attn {
     int causal, skip, window;
     float scale_log2;
     int tile, n_tiles;              // rows of a workgroup, workgroups over the rows of a sequence and key head
+    int z0;                         // the first of n_tiles * n_splits that a launch takes
     int group;                      // query heads of a key head
     uint32_t group_magic;           // row / group = row * group_magic >> 32 (0: a group of one)
     int n_splits, split_pages;      // a sequence's pages in pieces of split_pages, joined by a second launch where n_splits > 1
     float *partial, *partial_ml;    // [n_rows][n_heads][n_splits][dim] sums; [..][2] maximum (times scale, base 2) and denominator
 };
-bool kv4_attention_plan(Kv4Attn &a, bool is_f32);              // fills tile .. group_magic, n_splits, split_pages; false: too large for one launch
+bool kv4_attention_plan(Kv4Attn &a, bool is_f32);              // fills tile .. group_magic, n_splits, split_pages; false: too large
 size_t kv4_attention_workspace(const Kv4Attn &a);              // bytes of partial, for those
 template <typename T> void launch_kv4_attention(const Kv4Attn &a, hipStream_t s);
 

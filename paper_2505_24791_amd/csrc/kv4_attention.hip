@@ -161,7 +161,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && NG > 4 ? 1 : sizeof(T) == 4 
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, j = lane >> 4;
     const int G = a.group;
     // pieces further back come last: only long sequences have them
-    const int h = blockIdx.x, b = blockIdx.y, part = a.n_tiles == 1 ? blockIdx.z : blockIdx.z / a.n_tiles, tile = blockIdx.z - part * a.n_tiles;
+    const int z = blockIdx.z + a.z0;
+    const int h = blockIdx.x, b = blockIdx.y, part = a.n_tiles == 1 ? z : z / a.n_tiles, tile = z - part * a.n_tiles;
     const Seq sq = sequence(a, b);
     const int n_r = sq.n * G, r0 = tile * (kRows * NT);
     if (r0 >= n_r) return;
@@ -475,6 +476,8 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Attn a) {
 
 }  // namespace
 
+constexpr int kGridYZ = 65535;                    // workgroups of a grid's second and third dimension
+
 bool kv4_attention_plan(Kv4Attn &a, bool is_f32) {
     a.group = a.n_heads / a.cache.n_heads;
     a.group_magic = a.group > 1 ? (uint32_t)(((1ull << 32) + a.group - 1) / a.group) : 0u;
@@ -498,18 +501,16 @@ bool kv4_attention_plan(Kv4Attn &a, bool is_f32) {
     a.split_pages = per < 4 ? 4 : per;
     a.n_splits = (pages + a.split_pages - 1) / a.split_pages;
     if (a.n_splits < 1) a.n_splits = 1;
-    // the grid's second and third dimension, and rows for which group_magic is exact
-    return a.n_seqs <= 65535 && (int64_t)a.n_tiles * a.n_splits <= 65535 && rows * a.group < (int64_t)1 << 31 &&
-           (int64_t)a.n_seqs * a.n_heads * a.max_q <= INT32_MAX;
+    // the grid's second dimension, and rows for which group_magic is exact
+    return a.n_seqs <= kGridYZ && rows * a.group < (int64_t)1 << 31 && (int64_t)a.n_seqs * a.n_heads * a.max_q <= INT32_MAX;
 }
 
 size_t kv4_attention_workspace(const Kv4Attn &a) {
     return a.n_splits > 1 ? (size_t)a.n_rows * a.n_heads * a.n_splits * (a.cache.dim + 2) * sizeof(float) : 0;
 }
 
-template <typename T> void launch_kv4_attention(const Kv4Attn &a, hipStream_t s) {
-    if (a.n_rows <= 0 || a.n_seqs <= 0 || a.n_tiles <= 0) return;
-    const dim3 grid(a.cache.n_heads, a.n_seqs, a.n_tiles * a.n_splits), block(256);
+template <typename T> void launch_tiles(const Kv4Attn &a, int n, hipStream_t s) {
+    const dim3 grid(a.cache.n_heads, a.n_seqs, n), block(256);
     const int nt = a.tile / kRows;
 #define SJD_KV4_ATTEND(NG, NT) hipLaunchKernelGGL((kv4_attention_kernel<T, NG, NT>), grid, block, 0, s, a)
     if constexpr (sizeof(T) == 4) {
@@ -531,6 +532,14 @@ template <typename T> void launch_kv4_attention(const Kv4Attn &a, hipStream_t s)
         }
     }
 #undef SJD_KV4_ATTEND
+}
+
+template <typename T> void launch_kv4_attention(const Kv4Attn &a, hipStream_t s) {
+    if (a.n_rows <= 0 || a.n_seqs <= 0 || a.n_tiles <= 0) return;
+    const dim3 block(256);
+    const int all = a.n_tiles * a.n_splits;
+    Kv4Attn part = a;
+    for (part.z0 = 0; part.z0 < all; part.z0 += kGridYZ) launch_tiles<T>(part, all - part.z0 < kGridYZ ? all - part.z0 : kGridYZ, s);
     if (a.n_splits > 1) {
         const int64_t rows = (int64_t)a.n_seqs * a.n_heads * a.max_q;
         const bool wide = a.n_splits > 8;         // one round of requests for 16 lanes

@@ -1573,13 +1573,12 @@ int check_attention(const sjd_kv4 *c, const sjd_kv4_attention *g, Kv4Attn *out) 
     if (g->skip_nearest < 0 || g->window < 0) return fail(SJD_EINVAL, "skip_nearest and window must not be negative");
     if (!(g->scale > 0.f && isfinite(2.f * g->scale))) return fail(SJD_EINVAL, "scale must be above 0 and below 2^127");
     if (!g->q_start_dev && (int64_t)g->n_seqs * g->max_q != g->n_rows) return fail(SJD_EINVAL, "without q_start_dev there are n_seqs * max_q rows");
-    if ((int64_t)g->max_q * g->n_heads > INT32_MAX / 2 || g->max_kv > INT32_MAX / 2 || g->max_pages > INT32_MAX / SJD_KV4_PAGE ||
-        (int64_t)g->n_seqs * g->max_q > (int64_t)1 << 40)
+    a.max_q = g->max_q < g->n_rows ? g->max_q : g->n_rows;      // no sequence has more rows than there are
+    if ((int64_t)a.max_q * g->n_heads > INT32_MAX / 2 || g->max_kv > INT32_MAX / 2 || g->max_pages > INT32_MAX / SJD_KV4_PAGE)
         return fail(SJD_EINVAL, "max_q, max_kv or max_pages out of range");
     a.q = g->q_dev; a.o = g->o_dev; a.q_stride = g->q_stride; a.o_stride = g->o_stride; a.table_stride = g->table_stride;
     a.q_start = g->q_start_dev; a.kv_len = g->kv_len_dev; a.table = g->page_table_dev;
     a.n_seqs = g->n_seqs; a.n_heads = g->n_heads; a.n_rows = g->n_rows; a.max_pages = g->max_pages;
-    a.max_q = g->max_q < g->n_rows ? g->max_q : g->n_rows;      // no sequence has more rows than there are
     a.max_kv = (int)((int64_t)g->max_pages * SJD_KV4_PAGE < g->max_kv ? (int64_t)g->max_pages * SJD_KV4_PAGE : g->max_kv);
     a.causal = g->causal != 0;
     a.skip = g->skip_nearest < a.max_kv ? g->skip_nearest : a.max_kv;      // so many leave nothing; nothing overflows

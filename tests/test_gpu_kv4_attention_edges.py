@@ -72,3 +72,34 @@ def test_the_tail_of_a_softmax_with_one_leading_key(torch_cuda, name, sink, gap)
         assert torch.equal(got, got[:1].expand_as(got)), (seqs, rows)
         worst = (np.abs(_f64(got[:1]) - want) / bound).max()
         assert worst <= 1.0, (seqs, rows, worst)
+
+
+@pytest.mark.parametrize("name,rows,heads,dim,max_kv,window", [("float32", 131073, 8, 32, None, 50), ("float16", 262200, 8, 64, 20000, 0), ("bfloat16", 131073, 8, 256, None, 70)])
+def test_a_prompt_of_more_row_tiles_than_a_grid_counts(torch_cuda, name, rows, heads, dim, max_kv, window):
+    """65537 and more tiles of a key head's rows, against the bits of the same rows in calls of 8000.  With a window every row sees the keys before it,
+    without one all rows see the same hundred."""
+    import paper_2505_24791_amd as sjd
+    torch = torch_cuda
+    rng = np.random.default_rng(41)
+    n, cut = (rows, 8000) if window else (100, 8000)
+    g = torch.Generator(device="cuda").manual_seed(41)
+    pages = -(-n // 64)
+    dt = getattr(torch, name)
+    cache = sjd.Kv4Cache.zeros(pages, 1, dim, dt)
+    table = torch.from_numpy(rng.permutation(pages).astype(np.int32)).cuda()
+    t = torch.arange(n, device="cuda")
+    slot = (table[t // 64] * 64 + t % 64).to(torch.int32)
+    k, v = (torch.randn((n, 1, dim), generator=g, device="cuda").to(dt) for _ in range(2))
+    sjd.op_kv4_write(cache, k, v, slot)
+    wide = torch.nn.functional.pad(table, (0, 400)).view(1, -1)
+    q = torch.randn((rows, heads, dim), generator=g, device="cuda").to(dt)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    kw = dict(causal=bool(window), window=window)
+    got = sjd.op_kv4_attention(cache, q, wide, i32(n), q_start=i32(0, rows), max_q=rows, max_kv=max_kv or n, **kw)
+    for i in range(0, rows, cut):
+        part = q[i:i + cut]
+        m = len(part)
+        kv_len = i + m if window else n
+        want = sjd.op_kv4_attention(cache, part, wide, i32(kv_len), max_q=m, max_kv=max_kv or n, **kw)
+        assert torch.equal(got[i:i + m], want), i
+    assert not torch.equal(got[:8000], got[-8000:])
