@@ -9,8 +9,6 @@
 // of float32 here, and these kernels move bytes: each row is read once and written once.
 #include "kv4.h"
 
-#include <type_traits>
-
 namespace sjd {
 
 namespace {
@@ -85,14 +83,11 @@ template <typename T> __device__ __forceinline__ typename Vec<T, 4>::v round4(co
     return typename Vec<T, 4>::v{a[0], a[1], b[0], b[1]};
 }
 
-// Results of more than what the L2 caches hold (4 MB on each XCD) are stored past them: cold, 40000 tokens of 16 heads of 64 are read back in 32 us
-// that way and 53 through the caches, 32768 rows of 2 x 16 heads of 64 turned in 57 and 59.  Smaller ones stay for the call that comes next.
-constexpr int64_t kStreamBytes = 32 << 20;
-template <typename T, int N, bool STREAM> __device__ __forceinline__ void store(T *p, typename Vec<T, N>::v v) {
-    typename Vec<T, N>::v *d = reinterpret_cast<typename Vec<T, N>::v *>(p);
-    if constexpr (STREAM) __builtin_nontemporal_store(v, d);
-    else *d = v;
-}
+// Results go through the caches, however many: the call that reads them comes next.  Stores past the caches make a large call alone shorter (40000 tokens
+// of 16 heads of 64 read back: 32 us, 50 through them) and the pair of calls longer: 32768 rows of 2 x 16 heads of 64 into the cache and attended over 64
+// keys 229 us, 214 through the caches; turned, and queries and keys read once, 129 and 115; read back, and keys and values read once, 99 and 76.  From
+// 384 MB of results on, more than the last-level cache holds, the two are alike within 4% (512 MB: 403 and 399, 789 and 786, 298 and 309).
+template <typename T, int N> __device__ __forceinline__ void store(T *p, typename Vec<T, N>::v v) { *reinterpret_cast<typename Vec<T, N>::v *>(p) = v; }
 
 // Where a lane's two pieces of four channels begin: piece b holds the partners of piece a where the pairs are rot / 2 apart.
 struct Pieces { int a, b; };
@@ -177,7 +172,7 @@ constexpr int kThreads = 256;
 // length.  The 32768 rows into the cache (304 MB): 67 us.  Short calls are launch and one trip to memory: 32 rows 3.9 us.
 struct RopeShape { int per, log_step; double per_dim; };
 
-template <typename T, int L, bool WRITE, bool STREAM>
+template <typename T, int L, bool WRITE>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 5) void qk_rope_kernel(QkOpts o, QkRows r, Kv4Cache c, RopeShape sh) {
     typedef typename Vec<T, 4>::v v4;
     typedef typename Vec<T, 8>::v v8;
@@ -217,7 +212,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 5) void qk_rope_kern
     }
     __syncthreads();
     const double2 *turns = cs + row * pairs + i;
-    auto walk = [&](int h, int heads, const T *x, T *out, const float *gain, bool shifted, auto streamed, v4 a, v4 b) {
+    auto walk = [&](int h, int heads, const T *x, T *out, const float *gain, bool shifted, v4 a, v4 b) {
         const int64_t hop = (int64_t)step * r.dim;
         for (; h < heads; h += step) {
             asm volatile("" ::: "memory");       // factors are read from LDS for each head: kept in registers they would halve the waves
@@ -269,16 +264,16 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 5) void qk_rope_kern
                     for (int e = 0; e < 4; ++e) turn(y[e], y[4 + e], turns[e * quads]);
                 }
             }
-            store<T, 4, decltype(streamed)::value>(out + p.a, round4<T>(y));
-            store<T, 4, decltype(streamed)::value>(out + p.b, round4<T>(y + 4));
+            store<T, 4>(out + p.a, round4<T>(y));
+            store<T, 4>(out + p.b, round4<T>(y + 4));
             out += hop;
         }
     };
-    walk(h0, n_q, qx, (T *)r.q_out + at * r.q_out_stride + (int64_t)h0 * r.dim, affine, o.q_shift, std::bool_constant<STREAM>{}, qa, qb);
+    walk(h0, n_q, qx, (T *)r.q_out + at * r.q_out_stride + (int64_t)h0 * r.dim, affine, o.q_shift, qa, qb);
     if constexpr (!WRITE) {
-        walk(k0, n_k, kx, (T *)r.k_out + at * r.k_out_stride + (int64_t)k0 * r.dim, affine + r.dim, o.k_shift, std::bool_constant<STREAM>{}, ka, kb);
+        walk(k0, n_k, kx, (T *)r.k_out + at * r.k_out_stride + (int64_t)k0 * r.dim, affine + r.dim, o.k_shift, ka, kb);
     } else {
-        walk(k0, n_k, kx, keys + ((int64_t)row * r.n_kv + k0) * r.dim, affine + r.dim, o.k_shift, std::false_type{}, ka, kb);
+        walk(k0, n_k, kx, keys + ((int64_t)row * r.n_kv + k0) * r.dim, affine + r.dim, o.k_shift, ka, kb);
         constexpr int AHEAD = 4;                // values requested before the first is needed
         const T *vx = (const T *)r.v + at * r.v_stride + (int64_t)h0 * r.dim + 8 * i;
         v8 xv[AHEAD];
@@ -326,7 +321,7 @@ __global__ __launch_bounds__(kThreads) void kv4_write_kernel(QkRows r, Kv4Cache 
 // again into their L2 (40000 tokens of 16 heads of 64, cold, through the caches: 53 us, 60 with two rows of all heads a workgroup).  Bound by memory: 32 us
 // for those 207 MB, results stored past the caches; 3.8 us for 1000 scattered tokens.
 constexpr int kReadAhead = 2;
-template <typename T, bool STREAM>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4Cache c, const int32_t *slots, T *k, int64_t k_stride, T *v, int64_t v_stride,
                                                             int n_rows) {
     typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -362,7 +357,7 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4Cache c, const in
             const t2 x2 = __builtin_convertvector((f32x2)__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u][z], s, 2), t2);
             const t2 x3 = __builtin_convertvector((f32x2)__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w[u][z], s, 3), t2);
             T *out = (z ? v + row * v_stride : k + row * k_stride) + (int64_t)h * c.dim + 8 * ch;
-            store<T, 8, STREAM>(out, typename Vec<T, 8>::v{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]});
+            store<T, 8>(out, typename Vec<T, 8>::v{x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]});
         }
     }
 }
@@ -377,12 +372,10 @@ void launch_rope_lanes(const QkOpts &o, const QkRows &r, const Kv4Cache &c, hipS
     while (per > 1 && (per * heads > 8 * GROUPS || per > r.n_rows / 1024 || per * row_lds > 28672)) per /= 2;
     int log_step = 0;
     while (per << log_step < GROUPS) ++log_step;
-    const bool stream = (int64_t)r.n_rows * ((r.q ? r.n_heads : 0) + (r.k && !WRITE ? r.n_kv : 0)) * r.dim * (int64_t)sizeof(T) > kStreamBytes;
     const RopeShape sh{per, log_step, 1.0 / r.dim};
     const dim3 grid((r.n_rows + per - 1) / per), block(kThreads);
     const size_t lds = per * row_lds + 4 * r.dim * sizeof(float);
-    if (stream) hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE, true>), grid, block, lds, s, o, r, c, sh);
-    else hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE, false>), grid, block, lds, s, o, r, c, sh);
+    hipLaunchKernelGGL((qk_rope_kernel<T, L, WRITE>), grid, block, lds, s, o, r, c, sh);
 }
 
 template <typename T, bool WRITE>
@@ -411,10 +404,7 @@ template <typename T> void launch_kv4_read(const Kv4Cache &c, const int32_t *slo
     if (n_rows <= 0) return;
     const int rows = kThreads / (c.dim / 8) * kReadAhead;
     const dim3 grid((n_rows + rows - 1) / rows, c.n_heads), block(kThreads);
-    if (2 * (int64_t)n_rows * c.n_heads * c.dim * (int64_t)sizeof(T) > kStreamBytes)
-        hipLaunchKernelGGL((kv4_read_kernel<T, true>), grid, block, 0, s, c, slot, (T *)k, k_stride, (T *)v, v_stride, n_rows);
-    else
-        hipLaunchKernelGGL((kv4_read_kernel<T, false>), grid, block, 0, s, c, slot, (T *)k, k_stride, (T *)v, v_stride, n_rows);
+    hipLaunchKernelGGL((kv4_read_kernel<T>), grid, block, 0, s, c, slot, (T *)k, k_stride, (T *)v, v_stride, n_rows);
 }
 
 #define SJD_KV4_ROWS(T)                                                                                     \
