@@ -265,7 +265,7 @@ def _into(out, like, shape, dtype, what: str, device: int):
 
 
 def _ints(t, what: str, shape, device: int) -> int:
-    if t.dtype is not _rt[4] or t.get_device() != device or t.shape != shape or not t.is_contiguous():
+    if t is None or t.dtype is not _rt[4] or t.get_device() != device or t.shape != shape or not t.is_contiguous():
         _refuse(f"{what}: need a contiguous int32 tensor {tuple(shape)} on cuda:{device}")
     return t.data_ptr()
 

@@ -150,3 +150,12 @@ def test_counts_beyond_32_bits_are_refused(stub):
         with pytest.raises(sjd.SjdError):
             call()
     assert not stub.calls
+
+
+def test_a_rotation_without_positions_is_refused(stub):
+    o = sjd.QkOpts(rot_dim=64, axis_pairs=(32,), freq=Fake((32,), torch.float32))
+    x, cache = Fake((4, 2, 64), torch.float16), sjd.Kv4Cache(Fake((2, 2, 68 * 64), torch.uint8), torch.float16)
+    for call in (lambda: sjd.op_qk_norm_rope(x, None, None, o), lambda: sjd.op_kv4_write(cache, x, x, Fake((4,), torch.int32), opts=o)):
+        with pytest.raises(sjd.SjdError, match="pos"):
+            call()
+    assert not stub.calls
