@@ -320,7 +320,7 @@ SJD_API int sjd_op_kv4_read(const sjd_kv4 *cache, const int32_t *slot_dev, void 
  * on pages that the cache does not have are not seen.  Sums are held in float32, relative to a reference up to 2^8 below the largest
  * probability (IEEE half rows: 2^15): values over 2^96 can overflow them.  Probabilities are rounded to dtype (float32: not at all); those of IEEE half rows keep their
  * bits down to 2^-21 of the largest and are gone below 2^-32 of it.  A sequence's rows beyond max_q are left as they are, its keys beyond max_kv and
- * max_pages pages do not count; rows of no sequence are left as they are.
+ * max_pages pages do not count; rows of no sequence are left as they are.  o_dev may be q_dev (same stride), else they must not overlap.
  * Long sequences are cut in pieces that are joined in order in a second launch; how they are cut depends on the struct's numbers alone, and
  * the same call gives the same bits.  The pieces need a workspace (see below) that is the call's own until its work has ended. */
 typedef struct {

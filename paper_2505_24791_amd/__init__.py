@@ -452,7 +452,7 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
     """``sjd_op_kv4_attention``: q [rows, heads, head_dim], the last tokens of sequences with ``kv_len`` [seqs] int32 cached keys on the pages
     page_table [seqs, max_pages] int32; sequence b has the rows q_start[b] .. q_start[b+1] - 1 (q_start [seqs + 1] int32; None: max_q
     each).  max_q and max_kv bound the rows and keys of a sequence (max_kv None: all that the table has room for).  Rows of no
-    sequence are left as they are in ``out`` (None: a new tensor, which holds anything there)."""
+    sequence are left as they are in ``out`` (None: a new tensor, which holds anything there; ``q`` itself: in place)."""
     held, device = cache._now(), cache.device
     shape, q_stride = _rows3(q, "q", cache.dtype, device)
     n, heads, dim = shape

@@ -330,3 +330,22 @@ def test_calls_do_not_wait_for_another_stream(torch_cuda):
     early = not done.query()
     torch.cuda.synchronize()
     assert all(same) and early
+
+
+@pytest.mark.parametrize("name", TYPES)
+def test_results_in_the_place_of_the_queries(torch_cuda, name):
+    """Single tokens and a chunk, in pieces and whole, one and several tiles: the bits of a call with a result of its own."""
+    import paper_2505_24791_amd as sjd
+    torch = torch_cuda
+    rng = np.random.default_rng(48)
+    n, dim, H = 3000, 64, 6
+    k, v = (rng.choice([-3.0, -1.0, 0.5, 2.0], (n, 2, dim)) for _ in range(2))
+    cache, table = _cached(torch, sjd, name, k, v, rng)
+    for seqs, rows in ((3, 1), (1100, 1), (1, 100), (2, 1500)):
+        lens = torch.full((seqs,), n, dtype=torch.int32, device="cuda")
+        base = torch.from_numpy(rng.standard_normal((seqs * rows, H * dim + 5))).to(getattr(torch, name)).cuda()
+        q = base[:, 3:3 + H * dim].unflatten(1, (H, dim))
+        want = sjd.op_kv4_attention(cache, q.clone(), table.expand(seqs, -1), lens, max_q=rows)
+        pad = base[:, :3].clone()
+        assert sjd.op_kv4_attention(cache, q, table.expand(seqs, -1), lens, max_q=rows, out=q) is q
+        assert torch.equal(q, want) and torch.equal(base[:, :3], pad)
