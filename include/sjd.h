@@ -267,8 +267,8 @@ SJD_API int sjd_op_attention_h16(int dtype, const void *qkv_dev, void *o_dev, in
  * with gains and shifts [head_dim] float32 (NULL: 1 and 0; they need a norm).  The first rot_dim channels then turn in pairs:
  * pairing 0 takes channels (i, i + rot_dim / 2), pairing 1 takes (2 i, 2 i + 1), i < rot_dim / 2, and pair i turns by
  * position * freq_dev[i] radians, (a, b) -> (a cos - b sin, a sin + b cos).  The pairs are dealt to the axes in order, axis_pairs[a] of
- * them to axis a; each axis has a position of its own (any int32; |position * freq| below 2^50).  Everything in between is computed in float64 and
- * rounded once. */
+ * them to axis a; each axis has a position of its own (any int32; |position * freq| below 2^50).  Everything in between is computed in float64, then
+ * rounded to float32 and from there to dtype. */
 typedef struct {
     int32_t norm;                 /* 0, 1, 2 */
     float eps;                    /* >= 0 */

@@ -76,7 +76,7 @@ struct Kv4Attn {
     int group;                      // query heads of a key head
     uint32_t group_magic;           // row / group = row * group_magic >> 32 (0: a group of one)
     int n_splits, split_pages;      // a sequence's pages in pieces of split_pages, joined by a second launch where n_splits > 1
-    float *partial, *partial_ml;    // [n_rows][n_heads][n_splits][dim] sums; [..][2] maximum (times scale, base 2) and denominator
+    float *partial, *partial_ml;    // [n_rows][n_heads][n_splits][dim] sums; [..][2] reference (times scale, base 2) and denominator
 };
 bool kv4_attention_plan(Kv4Attn &a, bool is_f32);              // fills tile .. group_magic, n_splits, split_pages; false: too large
 size_t kv4_attention_workspace(const Kv4Attn &a);              // bytes of partial, for those

@@ -80,10 +80,11 @@ __device__ __forceinline__ void seen(const Kv4Attn &a, const Seq &s, int i, int 
 // 16 NT rows (new tokens times query heads of one key head) a workgroup, the pages of its piece of the sequence dealt to four
 // waves, each with its own maximum and sums, which are joined at the end.  S^T = K Q^T, 16 tokens an instruction: a lane holds row lane % 16 and, of a subtile, tokens 4 (lane / 16) + 0..3, which is
 // the right operand of O^T = V^T P^T as it stands, two subtiles to an instruction.
-// Single tokens are bound by the cache's bytes: 16 sequences of 20000 to 65536 keys, 8 key heads of 128 (743 MB), 148 us, 5.0 TB/s, and 6 to join;
-// 256 sequences of up to 1024 keys, 12 heads of 64 (108 MB), 25 us, of which 20 are bytes and the rest the longest sequence's workgroup.  Chunks of new
-// tokens are bound by the vector ALU (an exponential of 12 cycles a score, the conversion of the codes for every 32 rows) and by the uneven ends of
-// ragged sequences: 8 of up to 500 rows over 500 to 4000 keys, 16 heads of 64, 71 us, 230 TFLOP/s of the products that rows see.
+// Single tokens are bound by the cache's bytes: 16 sequences of 20000 to 65536 keys, 8 key heads of 128 (745 MB), 157 us a call with the join, 4.75 TB/s;
+// 256 sequences of up to 1024 keys, 12 heads of 64 (108 MB), 29 us, of which 20 are bytes and the rest the longest sequences' workgroups.  Chunks of new
+// tokens are bound by the vector ALU (an exponential of 12 cycles a score, the conversion of the codes for every 32 rows): 8 of 500 rows over 4000 keys, 16
+// heads of 64, 99 us, 620 TFLOP/s of the products that rows see; and by the uneven ends of ragged sequences: 8 of up to 500 rows over 500 to 4000 keys, 61
+// us, 270 TFLOP/s.  Whole prompts of 1024 tokens, 32 of them: 16 heads of 64 191 us, 360 TFLOP/s; 32 heads on 8 of 128 638 us, 431.
 // Registers hold what a page needs and nothing is shared through LDS before the end: pages converted once into LDS for four waves were no
 // faster on such sequences.
 constexpr int kRows = 16;

@@ -3,7 +3,7 @@
 //   y = x / sqrt(mean x^2 + eps) * gain      or      (x - mean) / sqrt(var + eps) * gain + shift      (over the channels of a head)
 //   (y_a, y_b) <- (y_a cos t - y_b sin t, y_b cos t + y_a sin t),   t = position[axis of the pair] * frequency[pair]
 //
-// Everything between the load and the one rounding to the rows' type is float64: a value that lands next to a border of the 4-bit
+// Everything between the load and the rounding (to float32, then to the rows' type) is float64: a value that lands next to a border of the 4-bit
 // grid then goes to the same side in whatever order sums are taken (float32 sums in another order move one key in ten million to
 // the next level, a third of its size), and angles of far positions keep their digits.  The vector unit does float64 at the rate
 // of float32 here, and these kernels move bytes: each row is read once and written once.
@@ -83,10 +83,11 @@ template <typename T> __device__ __forceinline__ typename Vec<T, 4>::v round4(co
     return typename Vec<T, 4>::v{a[0], a[1], b[0], b[1]};
 }
 
-// Results go through the caches, however many: the call that reads them comes next.  Stores past the caches make a large call alone shorter (40000 tokens
-// of 16 heads of 64 read back: 32 us, 50 through them) and the pair of calls longer: 32768 rows of 2 x 16 heads of 64 into the cache and attended over 64
-// keys 229 us, 214 through the caches; turned, and queries and keys read once, 129 and 115; read back, and keys and values read once, 99 and 76.  From
-// 384 MB of results on, more than the last-level cache holds, the two are alike within 4% (512 MB: 403 and 399, 789 and 786, 298 and 309).
+// Results go through the caches, however many: the call that reads them comes next.  Stores past the caches make a large call whose results nobody
+// reads shorter (32768 tokens of 16 heads of 64 read back: 27 us, 41 through them) and a call with its reader longer, in a row of such pairs on inputs that
+// change: those rows into the cache and attended over up to 1024 keys 251 us, 238 through the caches; 2 x 16 heads turned, and queries and keys read once, 109 and
+// 98; read back, and keys and values read once, 75 and 69.  From 512 MB of results on, more than the last-level cache holds, the two are alike within 4%
+// (385 and 384, 967 and 965, 295 and 304).
 template <typename T, int N> __device__ __forceinline__ void store(T *p, typename Vec<T, N>::v v) { *reinterpret_cast<typename Vec<T, N>::v *>(p) = v; }
 
 // Where a lane's two pieces of four channels begin: piece b holds the partners of piece a where the pairs are rot / 2 apart.
@@ -167,9 +168,9 @@ constexpr int kThreads = 256;
 // `step`-th head of it, so that addresses move by constants; the next head is requested under the present one's arithmetic.  cos and sin of every
 // (row, pair) are made once for all heads, in LDS.  WRITE: rounded keys go to LDS instead of memory, and with the values from there into
 // the cache.
-// Bound by memory: 32768 rows of 2 x 16 heads of 64 (268 MB in and out) take 56 us cold, 4.8 TB/s, where a copy of 2 GiB runs at 5.0; 47 us where the
-// rows come from the last-level cache.  9945 rows of 40 heads of 128, three axes (204 MB): 51 us, beside float64 arithmetic of much the same
-// length.  The 32768 rows into the cache (304 MB): 67 us.  Short calls are launch and one trip to memory: 32 rows 3.9 us.
+// Bound by memory: 32768 rows of 2 x 16 heads of 64 (268 MB in and out) take 58 us a call in a row of calls, 4.6 TB/s, where a copy of 2 GiB runs at
+// 5.0.  9945 rows of 40 heads of 128, three axes (204 MB): 55 us, beside float64 arithmetic of much the same length.  The 32768 rows into the cache
+// (304 MB): 75 us.  Short calls are launch and one trip to memory: 32 rows 4.0 us.
 struct RopeShape { int per, log_step; double per_dim; };
 
 template <typename T, int L, bool WRITE>
@@ -300,8 +301,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 4 ? 4 : 5) void qk_rope_kern
 }
 
 // Keys and values as they are: eight channels of a token's key and value a thread, one head of rows that follow one another a workgroup, so that what it
-// writes is the head's block of a page where the rows are its tokens (40000 tokens of 16 heads of 64, 207 MB, cold: 75 us, 89 with all heads of a row
-// side by side).  Requests for two or four rows at once (75) and value bytes exchanged between lanes for whole dwords (73) gave next to nothing.
+// writes is the head's block of a page where the rows are its tokens.  40000 tokens of 16 heads of 64, 207 MB: 50 us in a row of calls on changing inputs, 4.2
+// TB/s, and 61 in the kernel above (82 and 96 for scattered slots); right after a gigabyte of other writes 75, and 89 with all heads of a row side by
+// side.  Requests for two or four rows at once (75 there) and value bytes exchanged between lanes for whole dwords (73) gave next to nothing.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void kv4_write_kernel(QkRows r, Kv4Cache c) {
     typedef typename Vec<T, 8>::v v8;
@@ -318,8 +320,8 @@ __global__ __launch_bounds__(kThreads) void kv4_write_kernel(QkRows r, Kv4Cache 
 
 // Eight channels a thread, of a token's key and of its value; zeros for a slot outside the cache.  A workgroup takes one head of rows that follow
 // one another: where these are a page's tokens it reads the head's block of the page whole, which workgroups on other XCDs would otherwise read
-// again into their L2 (40000 tokens of 16 heads of 64, cold, through the caches: 53 us, 60 with two rows of all heads a workgroup).  Bound by memory: 32 us
-// for those 207 MB, results stored past the caches; 3.8 us for 1000 scattered tokens.
+// again into their L2 (40000 tokens of 16 heads of 64: 53 us, 60 with two rows of all heads a workgroup).  Bound by memory: 54 us for those 207 MB, 3.9
+// TB/s, four fifths of them writes; 4.4 us for 1000 scattered tokens.
 constexpr int kReadAhead = 2;
 template <typename T>
 __global__ __launch_bounds__(kThreads) void kv4_read_kernel(Kv4Cache c, const int32_t *slots, T *k, int64_t k_stride, T *v, int64_t v_stride,
