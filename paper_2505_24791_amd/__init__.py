@@ -249,8 +249,6 @@ def _rows3(t, what: str, dtype, device: int):
         _refuse(f"{what}: need a {dtype} tensor [rows, heads, head_dim] on cuda:{device}")
     if ((stride[1] != shape[2] and shape[1] != 1) or (stride[2] != 1 and shape[2] != 1)) and shape[0]:
         _refuse(f"{what}: the heads of a row must follow one another")
-    if shape[0] | shape[1] | shape[2] > _MOST:
-        _refuse(f"{what}: too many rows for one call")
     return shape, stride[0]
 
 
@@ -309,12 +307,12 @@ class QkOpts:
     def _take(self) -> None:
         """Checks the vectors and puts their addresses into the struct."""
         import torch
-        held = []
+        held, at = list(self.vectors.values()), []
         for name, t in self.vectors.items():
             if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 1):
                 _refuse(f"{name}: need a contiguous float32 vector on the GPU")
-            held.append((t, t.data_ptr()))
-            if t.numel() and not held[-1][1]:
+            at.append(t.data_ptr())
+            if t.numel() and not at[-1]:
                 _refuse(f"{name}: its memory has been freed")
         freq = self.vectors.get("freq")
         if freq is not None and freq.numel() != self.c.rot_dim // 2:
@@ -325,16 +323,14 @@ class QkOpts:
             _refuse("gains and shifts need one size, and all vectors one device")
         self.head_dim = sizes.pop() if sizes else None      # None: any
         self.device = devices.pop() if devices else None
-        for name, (_, at) in zip(self.vectors, held):
-            setattr(self.c, name, at)
-        self._held = held
+        for name, address in zip(self.vectors, at):
+            setattr(self.c, name, address)
+        self._held, self._at = held, at
 
     def _for(self, head_dim: int, device: int) -> int:
         """The struct's address, for rows of this head size on this device."""
-        for t, at in self._held:
-            if t.data_ptr() != at:                          # its storage was replaced: the old one may be anyone's by now
-                self._take()
-                break
+        if [t.data_ptr() for t in self._held] != self._at:  # a storage was replaced: the old one may be anyone's by now
+            self._take()
         if (self.head_dim is not None and self.head_dim != head_dim) or (self.device is not None and self.device != device):
             _refuse(f"the options hold vectors of {self.head_dim} values on cuda:{self.device}, the rows are of {head_dim} on cuda:{device}")
         return self.address
@@ -364,6 +360,8 @@ def op_qk_norm_rope(q, k, pos, opts: QkOpts, *, q_out=None, k_out=None):
         n, kh, dim = shape
         k_out, kos = _into(k_out, k, shape, dtype, "k_out", device)
         kp, ko = k.data_ptr(), k_out.data_ptr()
+    if n | qh | kh | dim > _MOST:
+        _refuse("too many rows for one call")
     p = _ints(pos, "pos", (n, opts.n_axes), device) if opts.n_axes else None
     _launch(device, _rt[0].sjd_op_qk_norm_rope, code, opts._for(dim, device), p, qp, qs, qh, kp, ks, kh, dim, qo, qos, ko, kos, n)
     return q_out, k_out
@@ -430,6 +428,8 @@ def op_kv4_write(cache: Kv4Cache, k, v, slot, *, opts: Optional[QkOpts] = None, 
             _refuse("q: other rows or another head size")
         q_out, qos = _into(q_out, q, shape, cache.dtype, "q_out", device)
         qp, heads, qo = q.data_ptr(), shape[1], q_out.data_ptr()
+    if n | heads > _MOST:
+        _refuse("too many rows for one call")
     _launch(device, _rt[0].sjd_op_kv4_write, to, sp, kp, ks, vp_, vs, n, op, pp, qp, qs, heads, qo, qos)
     return q_out if q is not None else None
 
@@ -462,13 +462,13 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
     if page_table.dtype is not _rt[4] or page_table.get_device() != device or len(table_shape) != 2 or (table_shape[1] > 1 and table_stride[1] != 1):
         _refuse(f"page_table: need int32 rows [seqs, max_pages] on cuda:{device}")
     seqs, pages = table_shape
-    if seqs | pages > _MOST:
-        _refuse("page_table: too many sequences or pages for one call")
     lens = _ints(kv_len, "kv_len", (seqs,), device)
     start = _ints(q_start, "q_start", (seqs + 1,), device) if q_start is not None else None
     out, out_stride = _into(out, q, shape, cache.dtype, "out", device)
     if max_kv is None:
         max_kv = pages * KV4_PAGE
+    if n | heads | seqs | pages > _MOST:
+        _refuse("too many rows, sequences or pages for one call")
     if not 0 <= max_q | max_kv | skip_nearest | window <= _MOST:
         _refuse("max_q, max_kv, skip_nearest and window are non-negative 32-bit integers")
     a = SjdKv4Attention(q.data_ptr(), out.data_ptr(), q_stride, out_stride, table_stride[0], start, lens, page_table.data_ptr(),
