@@ -349,3 +349,50 @@ def test_results_in_the_place_of_the_queries(torch_cuda, name):
         pad = base[:, :3].clone()
         assert sjd.op_kv4_attention(cache, q, table.expand(seqs, -1), lens, max_q=rows, out=q) is q
         assert torch.equal(q, want) and torch.equal(base[:, :3], pad)
+
+
+def test_a_gain_whose_storage_is_replaced(torch_cuda):
+    """``param.data = ...`` between two calls with the same options: the second reads the new values, in place of memory that is anyone's by then."""
+    import paper_2505_24791_amd as sjd
+    torch = torch_cuda
+    gain = torch.nn.Parameter(torch.full((64,), 2.0, device="cuda"))
+    opts = sjd.QkOpts(q_gain=gain, eps=0.0)
+    q = torch.ones((5, 3, 64), device="cuda")
+    assert bool((sjd.op_qk_norm_rope(q, None, None, opts)[0] == 2).all())
+    gain.data = torch.full((64,), 3.0, device="cuda")
+    other = [torch.full((64,), 7.0, device="cuda") for _ in range(8)]              # takes the old one's place
+    assert bool((sjd.op_qk_norm_rope(q, None, None, opts)[0] == 3).all()) and len(other) == 8
+    gain.data = gain.data.cpu()
+    with pytest.raises(sjd.SjdError):
+        sjd.op_qk_norm_rope(q, None, None, opts)
+
+
+def test_two_captured_graphs_replayed_at_once(torch_cuda):
+    """Two graphs over one cache, each with pieces to join, replayed side by side on two streams: a workspace belongs to one of them."""
+    import paper_2505_24791_amd as sjd
+    torch = torch_cuda
+    rng = np.random.default_rng(49)
+    n, dim, H = 20000, 128, 8
+    k, v = (rng.choice([-3.0, -1.0, 0.5, 2.0], (n, 2, dim)) for _ in range(2))
+    cache, table = _cached(torch, sjd, "bfloat16", k, v, rng)
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    qs = [torch.from_numpy(rng.standard_normal((1, H, dim))).bfloat16().cuda() for _ in range(2)]
+    sides, graphs, outs = [torch.cuda.Stream() for _ in qs], [], []
+    sjd.op_kv4_attention(cache, qs[0], table, lens)
+    torch.cuda.synchronize()
+    for q, side in zip(qs, sides):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=side):
+            outs.append(sjd.op_kv4_attention(cache, q, table, lens))
+    for seed in range(4):
+        for q in qs:
+            q.copy_(torch.from_numpy(rng.standard_normal((1, H, dim))))
+        want = [sjd.op_kv4_attention(cache, q, table, lens) for q in qs]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for graph, side in zip(graphs, sides):
+                with torch.cuda.stream(side):
+                    graph.replay()
+        torch.cuda.synchronize()
+        for got, w in zip(outs, want):
+            assert torch.equal(got, w), seed
