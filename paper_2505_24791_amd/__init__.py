@@ -579,22 +579,19 @@ class F8Rows:
         if n > _MOST:
             _refuse(f"{what}: too many rows for one call")
         a, b = codes.data_ptr(), scales.data_ptr()
-        self.device, self.n_rows, self._at = device, n, (a, b)
+        self.device, self.n_rows = device, n
         # a single row may have any stride: it has no next one
-        self._struct = s = _SJD_F8(a, b, stride[0], scale_stride[0], n, width) if n > 1 else _SJD_F8(a, b, padded, quads, n, width)
-        return s
+        return _SJD_F8(a, b, stride[0], scale_stride[0], n, width) if n > 1 else _SJD_F8(a, b, padded, quads, n, width)
 
     def _now(self, what: str) -> bytes:
-        """The struct, for the tensors as they are: a storage that was replaced is read where it is now."""
+        """The struct, for the tensors as they are.  Only that of a single allocation, whose tensors nobody has asked for, is kept: of a tensor in other hands a storage
+        may have been replaced, or its shape and strides in place."""
         both, s = self._both, self._struct                # read once: threads may share a weight
         if both is not None:
             if s is not None and both.data_ptr() == self._at:
                 return s
             self._parts()
-            s = None
-        if s is None or self._at != (self._codes.data_ptr(), self._scales.data_ptr()):
-            return self._take(what)
-        return s
+        return self._take(what)
 
     def _like(self):
         both = self._both

@@ -200,3 +200,25 @@ def test_projections_hand_over_what_they_were_given(stub):
     assert sjd.op_gated_mlp_f8(x, _rows(12), _rows(5, 6), activation="gelu", resid=r) is r
     assert stub.calls[-2][0] == "sjd_gated_mlp_f8_workspace" and stub.calls[-2][1][2] == sjd.DTYPE_F32
     assert stub.calls[-1][1][3:8] == (1, sjd.DTYPE_F32, 0x8000, 9, 1)
+
+
+def test_rows_whose_form_changes_in_place(stub):
+    """The tensors of the same addresses with other rows, strides or types: resized, or given another tensor's data that begins at the same place."""
+    r = _rows(50)
+    assert _struct(r._now("rows")) == (0x10000, 0x20000, 256, 4, 50, 200)
+    r.codes.shape, r.scales.shape = torch.Size((10, 256)), torch.Size((10, 4))
+    assert _struct(r._now("rows")) == (0x10000, 0x20000, 256, 4, 10, 200)
+    r.codes.steps, r.scales.steps = (512, 1), (8, 1)
+    assert _struct(r._now("rows")) == (0x10000, 0x20000, 512, 8, 10, 200)
+    with pytest.raises(sjd.SjdError, match="out"):
+        sjd.op_norm_f8(Alloc((50, 200), F16), out=r)
+    for change, back in ((dict(shape=torch.Size((10, 384))), dict(shape=torch.Size((10, 256)))), (dict(dtype=F16), dict(dtype=U8)), (dict(steps=(512, 2)), dict(steps=(512, 1))),
+                         (dict(device=1), dict(device=0))):
+        for name, value in change.items():
+            setattr(r.codes, name, value)
+        with pytest.raises(sjd.SjdError):
+            r._now("rows")
+        for name, value in back.items():
+            setattr(r.codes, name, value)
+        assert _struct(r._now("rows")) == (0x10000, 0x20000, 512, 8, 10, 200)
+    assert not stub.calls
