@@ -504,10 +504,10 @@ class F8Rows:
     ``width``, and ``scales`` uint8 [rows, groups of 128 rounded up to 4], a power of two 2^(byte - 127) for each 128 values.  Made by ``op_norm_f8`` (of a
     weight: ``norm="none"``) or held by the caller.  A call takes the tensors as they are then; rows of a larger tensor (``codes[a:b]``) are fine."""
 
-    __slots__ = ("_codes", "_scales", "_width", "_both", "_struct", "_at", "device", "n_rows")
+    __slots__ = ("_codes", "_scales", "_width", "_both", "_made", "device", "n_rows")
 
     def __init__(self, codes, scales, width: int):
-        self._codes, self._scales, self._width, self._both, self._struct = codes, scales, width, None, None
+        self._codes, self._scales, self._width, self._both = codes, scales, width, None
 
     @classmethod
     def empty(cls, n_rows: int, width: int, like):
@@ -522,17 +522,18 @@ class F8Rows:
         # codes and then scales in one allocation; tensors of them are made for whoever asks
         self._both = both = like.new_empty(n_rows * (padded + quads), dtype=rt[6])
         self._codes = self._scales = None
-        self._width, self.n_rows, self.device, self._at = width, n_rows, device, both.data_ptr()
-        self._struct = _SJD_F8(self._at, self._at + n_rows * padded, padded, quads, n_rows, width)
+        self._width, self.n_rows, self.device, at = width, n_rows, device, both.data_ptr()
+        self._made = at, _SJD_F8(at, at + n_rows * padded, padded, quads, n_rows, width), device, n_rows
         return self
 
     def _parts(self) -> None:
-        both, n, groups = self._both, self.n_rows, (self._width + 127) >> 7
+        both, groups = self._both, (self._width + 127) >> 7
         if both is None:                                  # another thread was here first
             return
+        n = self._made[3]
         codes, scales = both.split((n * (groups << 7), n * ((groups + 3) & ~3)))
         self._codes, self._scales = codes.view(n, groups << 7), scales.view(n, (groups + 3) & ~3)
-        self._struct, self._both = None, None
+        self._both = None
 
     @property
     def codes(self):
@@ -544,7 +545,7 @@ class F8Rows:
     def codes(self, tensor):
         if self._both is not None:
             self._parts()
-        self._codes, self._struct = tensor, None
+        self._codes = tensor
 
     @property
     def scales(self):
@@ -556,13 +557,13 @@ class F8Rows:
     def scales(self, tensor):
         if self._both is not None:
             self._parts()
-        self._scales, self._struct = tensor, None
+        self._scales = tensor
 
     @property
     def width(self) -> int:
         return self._width
 
-    def _take(self, what: str) -> bytes:
+    def _take(self, what: str):
         codes, scales, width, rt = self._codes, self._scales, self._width, _rt or _runtime()
         if type(width) is not int or not 1 <= width <= 1 << 20:
             _refuse(f"{what}: the width is an integer in 1..2^20")
@@ -581,21 +582,25 @@ class F8Rows:
         a, b = codes.data_ptr(), scales.data_ptr()
         self.device, self.n_rows = device, n
         # a single row may have any stride: it has no next one
-        return _SJD_F8(a, b, stride[0], scale_stride[0], n, width) if n > 1 else _SJD_F8(a, b, padded, quads, n, width)
+        return _SJD_F8(a, b, stride[0], scale_stride[0], n, width) if n > 1 else _SJD_F8(a, b, padded, quads, n, width), device, n, codes
 
-    def _now(self, what: str) -> bytes:
-        """The struct, for the tensors as they are.  Only that of a single allocation, whose tensors nobody has asked for, is kept: of a tensor in other hands a storage
-        may have been replaced, or its shape and strides in place."""
-        both, s = self._both, self._struct                # read once: threads may share a weight
+    def _form(self, what: str):
+        """(struct, device, number of rows, a tensor of that device) of the tensors as they are, of one look: threads may share a weight, and one of them may replace it.
+        Only the struct of a single allocation, whose tensors nobody has asked for, is kept: of a tensor in other hands a storage may have been replaced, or its
+        shape and strides in place."""
+        both = self._both
         if both is not None:
-            if s is not None and both.data_ptr() == self._at:
-                return s
+            at, struct, device, n = self._made
+            if both.data_ptr() == at:
+                return struct, device, n, both
             self._parts()
         return self._take(what)
 
+    def _now(self, what: str) -> bytes:
+        return self._form(what)[0]
+
     def _like(self):
-        both = self._both
-        return self._codes if both is None else both
+        return self._form("rows")[3]
 
 
 def _rows2(t, what: str, device: int):
@@ -644,10 +649,10 @@ def op_norm_f8(x, *, resid=None, norm: Optional[str] = "rms", gain=None, shift=N
         sp = _vector(shift, "shift", width, device)
     if out is None:
         out = F8Rows.empty(n, width, x)
-        to = out._struct
+        to = out._made[1]
     else:
-        to = out._now("out")
-        if out.device != device or out.n_rows != n or out._width != width:
+        to, on, rows, _ = out._form("out")
+        if on != device or rows != n or out._width != width:
             _refuse(f"out: need {n} rows of {width} on cuda:{device}")
     _launch(device, _rt[0].sjd_op_norm_f8, code, x.data_ptr(), stride, rcode, rp, rs, kind, eps, gp, sp, to)
     return out
@@ -655,51 +660,51 @@ def op_norm_f8(x, *, resid=None, norm: Optional[str] = "rms", gain=None, shift=N
 
 def op_f8_read(rows: F8Rows, dtype, *, out=None):
     """``sjd_op_f8_read``: the values [rows, width] of 8-bit rows in ``dtype`` (float16, bfloat16 or float32); ``out`` or a new tensor."""
-    held, code = rows._now("rows"), _row_dtype(dtype)
-    out, stride = _result(rows, rows._width, dtype, out, "out")
-    _launch(rows.device, _rt[0].sjd_op_f8_read, held, code, out.data_ptr(), stride)
+    (held, device, n, like), code = rows._form("rows"), _row_dtype(dtype)
+    out, stride = _result(like, device, n, rows._width, dtype, out, "out")
+    _launch(device, _rt[0].sjd_op_f8_read, held, code, out.data_ptr(), stride)
     return out
 
 
-def _result(rows: F8Rows, outs: int, dtype, out, what: str):
-    """(result [rows, outs], its row stride): a new tensor, or the one that the caller gave, checked."""
+def _result(like, device: int, n: int, outs: int, dtype, out, what: str):
+    """(result [n, outs], its row stride): a new tensor, or the one that the caller gave, checked."""
     if out is None:
-        return rows._like().new_empty((rows.n_rows, outs), dtype=dtype), outs
+        return like.new_empty((n, outs), dtype=dtype), outs
     if out.dtype is not dtype:
         _refuse(f"{what}: need a {dtype} tensor")
-    got, stride = _rows2(out, what, rows.device)
-    if got != (rows.n_rows, outs):
-        _refuse(f"{what}: need the shape {(rows.n_rows, outs)}")
+    got, stride = _rows2(out, what, device)
+    if got != (n, outs):
+        _refuse(f"{what}: need the shape {(n, outs)}")
     return out, stride
 
 
-def _projected(rows: F8Rows, outs: int, dtype, resid, out):
+def _projected(like, device: int, n: int, outs: int, dtype, resid, out):
     """(result, its row stride, dtype code, accumulate) of a projection: new rows of dtype (float16 unless given), `out`, or added to the float32 `resid`."""
     if resid is not None:
         if out is not None or (dtype is not None and _row_dtype(dtype) != DTYPE_F32) or _row_dtype(resid.dtype) != DTYPE_F32:
             _refuse("with resid the result is added to it, in float32")
-        out, stride = _result(rows, outs, resid.dtype, resid, "resid")
+        out, stride = _result(like, device, n, outs, resid.dtype, resid, "resid")
         return out, stride, DTYPE_F32, 1
     if dtype is None:
         dtype = _rt[8] if out is None else out.dtype
     code = _row_dtype(dtype)
-    out, stride = _result(rows, outs, dtype, out, "out")
+    out, stride = _result(like, device, n, outs, dtype, out, "out")
     return out, stride, code, 0
 
 
 def op_linear_f8(rows: F8Rows, weight: F8Rows, *, bias=None, resid=None, dtype=None, out=None):
     """``sjd_op_linear_f8``: rows times weight [outputs, inputs] plus bias [outputs] float32: a new tensor [rows, outputs] of ``dtype`` (float16 unless
     given), or ``out``; with ``resid`` [rows, outputs] float32 the result is added to it in place."""
-    x, w, device, outs = rows._now("rows"), weight._now("weight"), rows.device, weight.n_rows
-    if weight.device != device:
+    (x, device, n, like), (w, w_device, outs, _) = rows._form("rows"), weight._form("weight")
+    if w_device != device:
         _refuse("rows and weight must be on one GPU")
     bp = None if bias is None else _vector(bias, "bias", outs, device)
     if resid is None and out is None:
         if dtype is None:
             dtype = _rt[8]
-        code, accumulate, stride, out = _row_dtype(dtype), 0, outs, rows._like().new_empty((rows.n_rows, outs), dtype=dtype)
+        code, accumulate, stride, out = _row_dtype(dtype), 0, outs, like.new_empty((n, outs), dtype=dtype)
     else:
-        out, stride, code, accumulate = _projected(rows, outs, dtype, resid, out)
+        out, stride, code, accumulate = _projected(like, device, n, outs, dtype, resid, out)
     _launch(device, _rt[0].sjd_op_linear_f8, x, w, bp, code, out.data_ptr(), stride, accumulate)
     return out
 
@@ -707,18 +712,18 @@ def op_linear_f8(rows: F8Rows, weight: F8Rows, *, bias=None, resid=None, dtype=N
 def op_gated_mlp_f8(rows: F8Rows, w_in: F8Rows, w_out: F8Rows, *, activation: str = "silu", resid=None, dtype=None, out=None):
     """``sjd_op_gated_mlp_f8``: the gated feed-forward block, activation(rows gate^T) * (rows up^T) in 8 bits, times w_out^T.  w_in: the
     rows of the gate, then those of up; ``activation``: "silu" or "gelu"; ``resid``, ``dtype`` and ``out`` as for ``op_linear_f8``."""
-    x, wi, wo, device = rows._now("rows"), w_in._now("w_in"), w_out._now("w_out"), rows.device
-    if w_in.device != device or w_out.device != device:
+    (x, device, n, like), (wi, wi_device, _, _), (wo, wo_device, outs, _) = rows._form("rows"), w_in._form("w_in"), w_out._form("w_out")
+    if wi_device != device or wo_device != device:
         _refuse("rows and weights must be on one GPU")
     act = _ACTIVATIONS.get(activation)
     if act is None:
         _refuse(f"activation must be one of {list(_ACTIVATIONS)}")
     lib, need = _rt[0], C.c_size_t()
-    out, stride, code, accumulate = _projected(rows, w_out.n_rows, dtype, resid, out)
+    out, stride, code, accumulate = _projected(like, device, n, outs, dtype, resid, out)
     rc = lib.sjd_gated_mlp_f8_workspace(x, wi, code, C.addressof(need))
     if rc:
         _check(rc)
-    workspace = rows._like().new_empty(need.value, dtype=_rt[6])
+    workspace = like.new_empty(need.value, dtype=_rt[6])
     _launch(device, lib.sjd_op_gated_mlp_f8, x, wi, wo, act, code, out.data_ptr(), stride, accumulate, workspace.data_ptr(), need.value)
     return out
 

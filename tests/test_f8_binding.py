@@ -222,3 +222,32 @@ def test_rows_whose_form_changes_in_place(stub):
             setattr(r.codes, name, value)
         assert _struct(r._now("rows")) == (0x10000, 0x20000, 512, 8, 10, 200)
     assert not stub.calls
+
+
+def test_a_call_sees_one_form_of_rows_that_another_thread_replaces(stub, monkeypatch):
+    """The struct, the device and the number of rows that a call goes by are of one look: another thread replaces the tensors and looks at them in the middle of it."""
+    class There(Alloc):
+        def new_empty(self, shape, dtype=None):
+            return There((shape,) if isinstance(shape, int) else shape, dtype or self.dtype, 0x900000, device=self.device)
+
+    pack = sjd._SJD_F8
+    r = _rows(9)
+
+    def while_another_thread_replaces(*values):
+        if values[4] == 9:
+            monkeypatch.setattr(sjd, "_SJD_F8", pack)
+            r.codes, r.scales = There((3, 256), U8, 0x70000, device=1), There((3, 4), U8, 0x80000, device=1)
+            assert _struct(r._now("rows")) == (0x70000, 0x80000, 256, 4, 3, 200)
+        return pack(*values)
+
+    def start():
+        r.codes, r.scales = There((9, 256), U8), There((9, 4), U8, 0x20000)
+        monkeypatch.setattr(sjd, "_SJD_F8", while_another_thread_replaces)
+
+    for call, shape in ((lambda: sjd.op_f8_read(r, F16), (9, 200)), (lambda: sjd.op_linear_f8(r, _rows(5)), (9, 5)), (lambda: sjd.op_linear_f8(r, _rows(5), out=Alloc((9, 5), F16)), (9, 5)),
+                        (lambda: sjd.op_linear_f8(_rows(2), r), (2, 9)), (lambda: sjd.op_gated_mlp_f8(r, _rows(12), _rows(5, 6)), (9, 5))):
+        start()
+        out = call()
+        assert tuple(out.shape) == shape and out.device == 0
+    start()
+    assert sjd.op_norm_f8(Alloc((9, 200), F16), out=r) is r and _struct(stub.calls[-1][1][10])[4] == 9
