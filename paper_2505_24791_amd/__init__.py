@@ -504,7 +504,7 @@ class F8Rows:
     ``width``, and ``scales`` uint8 [rows, groups of 128 rounded up to 4], a power of two 2^(byte - 127) for each 128 values.  Made by ``op_norm_f8`` (of a
     weight: ``norm="none"``) or held by the caller.  A call takes the tensors as they are then; rows of a larger tensor (``codes[a:b]``) are fine."""
 
-    __slots__ = ("_codes", "_scales", "_width", "_both", "_made", "device", "n_rows")
+    __slots__ = ("_codes", "_scales", "_width", "_both", "_made")
 
     def __init__(self, codes, scales, width: int):
         self._codes, self._scales, self._width, self._both = codes, scales, width, None
@@ -522,7 +522,7 @@ class F8Rows:
         # codes and then scales in one allocation; tensors of them are made for whoever asks
         self._both = both = like.new_empty(n_rows * (padded + quads), dtype=rt[6])
         self._codes = self._scales = None
-        self._width, self.n_rows, self.device, at = width, n_rows, device, both.data_ptr()
+        self._width, at = width, both.data_ptr()
         self._made = at, _SJD_F8(at, at + n_rows * padded, padded, quads, n_rows, width), device, n_rows
         return self
 
@@ -563,6 +563,14 @@ class F8Rows:
     def width(self) -> int:
         return self._width
 
+    @property
+    def n_rows(self) -> int:
+        return self._made[3] if self._both is not None else self._codes.shape[0]
+
+    @property
+    def device(self) -> int:
+        return self._made[2] if self._both is not None else self._codes.get_device()
+
     def _take(self, what: str):
         codes, scales, width, rt = self._codes, self._scales, self._width, _rt or _runtime()
         if type(width) is not int or not 1 <= width <= 1 << 20:
@@ -580,7 +588,6 @@ class F8Rows:
         if n > _MOST:
             _refuse(f"{what}: too many rows for one call")
         a, b = codes.data_ptr(), scales.data_ptr()
-        self.device, self.n_rows = device, n
         # a single row may have any stride: it has no next one
         return _SJD_F8(a, b, stride[0], scale_stride[0], n, width) if n > 1 else _SJD_F8(a, b, padded, quads, n, width), device, n, codes
 

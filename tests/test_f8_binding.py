@@ -251,3 +251,16 @@ def test_a_call_sees_one_form_of_rows_that_another_thread_replaces(stub, monkeyp
         assert tuple(out.shape) == shape and out.device == 0
     start()
     assert sjd.op_norm_f8(Alloc((9, 200), F16), out=r) is r and _struct(stub.calls[-1][1][10])[4] == 9
+
+
+def test_rows_say_how_many_they_are_and_where_before_any_call(stub):
+    r = _rows(5, device=1)
+    assert r.n_rows == 5 and r.device == 1
+    r.codes, r.scales = Alloc((7, 256), U8), Alloc((7, 4), U8)
+    assert r.n_rows == 7 and r.device == 0
+    x = torch.zeros(3, 200)
+    x.get_device = lambda: 0
+    made = sjd.F8Rows.empty(3, 200, x)
+    assert made.n_rows == 3 and made.device == 0
+    made.codes = Alloc((9, 256), U8, device=2)
+    assert made.n_rows == 9 and made.device == 2
