@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 import struct
+import threading
 from dataclasses import dataclass
 from typing import Optional, Tuple
 
@@ -497,6 +498,7 @@ def op_kv4_attention(cache: Kv4Cache, q, page_table, kv_len, *, q_start=None, ma
 F8_GROUP = 128         # values that share a scale in 8-bit rows
 _SJD_F8 = struct.Struct("PPqqii").pack      # sjd_f8; a call takes the bytes as they are: a ctypes structure takes 0.4 us longer to make
 _ACTIVATIONS = {"silu": 0, "gelu": 1}
+_parting = threading.Lock()
 
 
 class F8Rows:
@@ -527,13 +529,14 @@ class F8Rows:
         return self
 
     def _parts(self) -> None:
-        both, groups = self._both, (self._width + 127) >> 7
-        if both is None:                                  # another thread was here first
-            return
-        n = self._made[3]
-        codes, scales = both.split((n * (groups << 7), n * ((groups + 3) & ~3)))
-        self._codes, self._scales = codes.view(n, groups << 7), scales.view(n, (groups + 3) & ~3)
-        self._both = None
+        with _parting:                                    # or tensors that one thread has set are lost under those that another still makes
+            both, groups = self._both, (self._width + 127) >> 7
+            if both is None:                              # another thread was here first
+                return
+            n = self._made[3]
+            codes, scales = both.split((n * (groups << 7), n * ((groups + 3) & ~3)))
+            self._codes, self._scales = codes.view(n, groups << 7), scales.view(n, (groups + 3) & ~3)
+            self._both = None
 
     @property
     def codes(self):

@@ -264,3 +264,38 @@ def test_rows_say_how_many_they_are_and_where_before_any_call(stub):
     assert made.n_rows == 3 and made.device == 0
     made.codes = Alloc((9, 256), U8, device=2)
     assert made.n_rows == 9 and made.device == 2
+
+
+def test_tensors_set_while_another_thread_asks_for_the_made_ones_stay(stub):
+    """Making tensors of the parts takes a while; what another thread sets meanwhile is not lost, and all who ask get the same tensors."""
+    import threading
+    for use in ("set", "ask"):
+        inside, go_on, went = threading.Event(), threading.Event(), []
+
+        class Slow(torch.Tensor):
+            def split(self, sizes):
+                first, inside_before = not inside.is_set(), inside.set()
+                if first:
+                    go_on.wait(0.5)
+                return torch.Tensor.split(self, sizes)
+
+        x = torch.zeros(3, 200)
+        x.get_device = lambda: 0
+        r = sjd.F8Rows.empty(3, 200, x)
+        r._both = r._both.as_subclass(Slow)
+        mine = Alloc((3, 256), U8, 0x70000)
+
+        def second():
+            inside.wait(5)
+            if use == "set":
+                r.codes = mine
+            went.append(r.codes)
+            go_on.set()
+
+        one, two = threading.Thread(target=lambda: went.append(r.scales)), threading.Thread(target=second)
+        one.start(), two.start(), one.join(), two.join()
+        assert len(went) == 2
+        if use == "set":
+            assert r.codes is mine
+        else:
+            assert any(t is r.codes for t in went) and any(t is r.scales for t in went)
