@@ -320,8 +320,8 @@ class QkOpts:
         for name, t in self.vectors.items():
             if not (t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.dim() == 1):
                 _refuse(f"{name}: need a contiguous float32 vector on the GPU")
-            at.append(t.data_ptr())
-            if t.numel() and not at[-1]:
+            at.append((t.data_ptr(), t.shape, t.stride()))
+            if t.numel() and not at[-1][0]:
                 _refuse(f"{name}: its memory has been freed")
         freq = self.vectors.get("freq")
         if freq is not None and freq.numel() != self.c.rot_dim // 2:
@@ -332,13 +332,14 @@ class QkOpts:
             _refuse("gains and shifts need one size, and all vectors one device")
         self.head_dim = sizes.pop() if sizes else None      # None: any
         self.device = devices.pop() if devices else None
-        for name, address in zip(self.vectors, at):
+        for name, (address, _, _) in zip(self.vectors, at):
             setattr(self.c, name, address)
         self._held, self._at = held, at
 
     def _for(self, head_dim: int, device: int) -> int:
         """The struct's address, for rows of this head size on this device."""
-        if [t.data_ptr() for t in self._held] != self._at:  # a storage was replaced: the old one may be anyone's by now
+        # a storage that was replaced may be anyone's by now, and one that was kept may have another size
+        if [(t.data_ptr(), t.shape, t.stride()) for t in self._held] != self._at:
             self._take()
         if (self.head_dim is not None and self.head_dim != head_dim) or (self.device is not None and self.device != device):
             _refuse(f"the options hold vectors of {self.head_dim} values on cuda:{self.device}, the rows are of {head_dim} on cuda:{device}")
@@ -394,12 +395,14 @@ class Kv4Cache:
         self.device = pages.get_device()
         self.n_pages, self.kv_heads, self.head_dim = pages.shape[0], pages.shape[1], pages.shape[2] // 68
         c = self.c
-        self._from, self._at = pages, pages.data_ptr()
-        c.pages, c.n_pages, c.n_kv_heads, c.head_dim = self._at, self.n_pages, self.kv_heads, self.head_dim
+        self._from, self._at = pages, (pages.data_ptr(), pages.shape, pages.stride())
+        c.pages, c.n_pages, c.n_kv_heads, c.head_dim = self._at[0], self.n_pages, self.kv_heads, self.head_dim
 
     def _now(self) -> int:
         """The struct's address, for the pages as they are."""
-        if self.pages is not self._from or self._from.data_ptr() != self._at:      # replaced: the old memory may be anyone's by now
+        pages = self.pages
+        # replaced: the old memory may be anyone's by now; or of another form in place
+        if pages is not self._from or (pages.data_ptr(), pages.shape, pages.stride()) != self._at:
             self._take()
         return self.address
 

@@ -159,3 +159,30 @@ def test_a_rotation_without_positions_is_refused(stub):
         with pytest.raises(sjd.SjdError, match="pos"):
             call()
     assert not stub.calls
+
+
+def test_options_and_caches_whose_tensors_change_form_in_place(stub):
+    """Vectors and pages of the same address with another shape or stride: resized, or given another tensor's data that begins at the same place."""
+    gain, x = Fake((64,), torch.float32, 0x1000), Fake((4, 2, 64), torch.float16)
+    opts = sjd.QkOpts(norm="rms", q_gain=gain, k_gain=gain)
+    sjd.op_qk_norm_rope(x, x, None, opts)
+    stub.calls.clear()
+    gain.shape = torch.Size((32,))
+    with pytest.raises(sjd.SjdError, match="32"):
+        sjd.op_qk_norm_rope(x, x, None, opts)
+    gain.shape, gain.is_contiguous, gain.steps = torch.Size((64,)), (lambda: False), (2,)
+    with pytest.raises(sjd.SjdError, match="contiguous"):
+        sjd.op_qk_norm_rope(x, x, None, opts)
+    pages = Fake((10, 2, 68 * 64), torch.uint8, 0x5000)
+    cache = sjd.Kv4Cache(pages, torch.float16)
+    k, slot = Fake((3, 2, 64), torch.float16), Fake((3,), torch.int32)
+    sjd.op_kv4_write(cache, k, k, slot)
+    assert _struct(stub.calls[-1][1][0], sjd.SjdKv4).n_pages == 10
+    pages.shape = torch.Size((4, 2, 68 * 64))
+    sjd.op_kv4_write(cache, k, k, slot)
+    assert _struct(stub.calls[-1][1][0], sjd.SjdKv4).n_pages == 4 and cache.n_pages == 4
+    stub.calls.clear()
+    pages.is_contiguous, pages.steps = (lambda: False), (1 << 20, 68 * 64, 1)
+    with pytest.raises(sjd.SjdError, match="contiguous"):
+        sjd.op_kv4_write(cache, k, k, slot)
+    assert not stub.calls
