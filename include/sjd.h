@@ -381,7 +381,8 @@ SJD_API int sjd_op_linear_f8(const sjd_f8 *rows, const sjd_f8 *weight, const flo
                              int accumulate, void *hip_stream);
 
 /* The gated feed-forward block: w_in holds the F rows of the gate and then the F of `up`, hidden = activation(rows gate^T) * (rows up^T) is held in 8 bits, and
- * c_dev [rows->n_rows, w_out->n_rows] = hidden w_out^T as sjd_op_linear_f8 gives it; w_out->width = F <= 32768.  activation 0: x * sigmoid(x), 1: GELU (erf form).
+ * c_dev [rows->n_rows, w_out->n_rows] = hidden w_out^T as sjd_op_linear_f8 gives it; w_out->width = F <= 32768.  activation 0: x * sigmoid(x), 1: GELU (erf form), each within
+ * 1e-5 of itself down to where sigmoid(x) or the normal distribution function is 2^-126, zero below.
  * The workspace, on a 16-byte boundary, is the call's own until its work has ended. */
 SJD_API int sjd_op_gated_mlp_f8(const sjd_f8 *rows, const sjd_f8 *w_in, const sjd_f8 *w_out, int activation, int dtype, void *c_dev, int64_t c_stride,
                                 int accumulate, void *workspace_dev, size_t workspace_bytes, void *hip_stream);

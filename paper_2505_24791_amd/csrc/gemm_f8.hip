@@ -57,9 +57,26 @@ void allow_lds(const void *kern, int bytes, std::atomic<uint64_t> &allowed) {
     if (hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess) allowed.fetch_or(bit, std::memory_order_release);
 }
 
-// Activations of the gated block, on float32 sums that are rounded to 4 bits of mantissa afterwards.
+// GELU (erf form) whose error is relative: gelu(v) = max(v, 0) - |v| Phi(-|v|), Phi(-t) = exp(-t^2 / 2) R(t), and R is a polynomial of degree 8 without a constant in w = 1 / (1 + 0.3 t), fitted
+// to 9.2e-8 of it on 0 <= t <= 13.5 (1 / t beyond, as R has it).  128 channels share a scale that follows the largest of them, so a group whose gates all lie in the tail is held with all its
+// bits: gelu_erf_h16, whose bound is absolute, is off by 0.6% at -5 and 8% at -6 there, a step of the grid.  Evaluated in float32: 1.4e-6 down to -5, 8e-6 to -13, what the exponent is rounded by; below,
+// where Phi is under 2^-126, zero.  The minimum with 16 keeps |v| Phi of +inf from being inf * 0; a NaN stays one.  The block with 16384 x 1024, 2816 hidden 146 -> 148 us, 300 x 1408, 3841 hidden 25.2 both.
+__device__ __forceinline__ float gelu_tail(float v) {
+    const float t = fabsf(__builtin_elementwise_minimum(v, 16.f));
+    const float w = __builtin_amdgcn_rcpf(fmaf(0.3f, t, 1.f));
+    float p = fmaf(0.0359241813f, w, -0.158233225f);
+    p = fmaf(p, w, 0.208106712f);
+    p = fmaf(p, w, -0.0552709624f);
+    p = fmaf(p, w, 0.129383847f);
+    p = fmaf(p, w, 0.0996707305f);
+    p = fmaf(p, w, 0.120791711f);
+    p = fmaf(p, w, 0.119626909f);
+    return fmaf(-t * (p * w), __builtin_amdgcn_exp2f(-0.72134752f * t * t), fmaxf(v, 0.f));
+}
+
+// Activations of the gated block, on float32 sums that are rounded to 4 bits of mantissa afterwards, relative to the largest of 128.
 __device__ __forceinline__ float gate_of(float g, int act) {
-    if (act) return gelu_erf_h16(g);
+    if (act) return gelu_tail(g);
     return g * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * g));
 }
 

@@ -1,0 +1,57 @@
+"""The gated block of 8-bit rows where its hidden values are easily wrong: gates in the tail of the activation.
+
+Tolerances.  Hidden values lie on a grid of 8-bit floats: half a step, 2^-4 of a value or 2^-10 of a scale (at least the group's largest / 448).  The activation's float32 arithmetic
+is off by what the exponent of 2 is rounded by, 2^-24 of it twice and 2^-25 for its constant (it is at most 116 for the gates here: 2.5 * 116 * 2^-24 ln 2 < 2^-16), and by less than 2^-18 for the rest.
+Sums of integers are exact.
+"""
+import pytest
+import torch
+
+import f8_reference as ref
+import paper_2505_24791_amd as sjd
+from test_gpu_f8 import BF16, F32, _gen, _rows
+
+pytestmark = pytest.mark.gpu
+
+# rows, width, hidden channels: each launch that the gate has (few rows, few rows with long k, tiles, and tiles that fill the chip)
+LAUNCHES = [(5, 200, 256), (40, 1100, 640), (400, 1100, 1280), (3000, 300, 640), (9000, 300, 2304)]
+
+
+def _picked(hidden, n, g):
+    """A weight that picks n hidden channels, so that what is held is seen as it is."""
+    pick = torch.randint(0, hidden, (n,), generator=g)
+    w = torch.zeros(n, hidden)
+    w[torch.arange(n), pick] = 1
+    return pick, _rows(*ref.hold(w), hidden)
+
+
+@pytest.mark.parametrize("m,width,hidden", LAUNCHES)
+@pytest.mark.parametrize("act,low,high", [("gelu", -8.0, -4.0), ("gelu", -12.0, -8.0), ("gelu", -4.0, 4.0), ("silu", -16.0, -8.0), ("silu", -80.0, -64.0), ("silu", -4.0, 4.0)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_group_of_gates_in_the_tail_keeps_its_bits(m, width, hidden, act, low, high, dtype):
+    """All gates of 128 channels lie between `low` and `high`: their hidden values are held by a scale of their own, so each has to be right relative to itself."""
+    g = _gen(hidden)
+    # a row is (1, 2^-4, zeros): a gate is a + b / 16 with two values of the grid, exactly
+    x = torch.zeros(m, width)
+    x[:, 0], x[:, 1] = 1.0, 0.0625
+    step = (high - low) / 16
+    gate = torch.zeros(hidden, width)
+    gate[:, 0] = low + step * torch.randint(0, 16, (hidden,), generator=g)
+    gate[:, 1] = step * torch.randint(0, 15, (hidden,), generator=g)
+    gate = ref.values(*ref.hold(gate), width).float()                      # as the grid has them
+    up = torch.zeros(hidden, width)
+    up[:, 0] = 1.0
+    z = (x[:1].double() @ gate.double().T)[0]
+    assert float(z.min()) >= low - abs(low) / 16 and float(z.max()) <= high + abs(high) / 8 + 1
+    h = ref.activation(z, act)
+    top = torch.nn.functional.pad(h.abs(), (0, -hidden % 128)).view(-1, 128).amax(-1)
+    grid = 2.0 ** -10 * torch.repeat_interleave(torch.exp2(torch.ceil(torch.log2(top * (1 + 2.0 ** -16) / 448))), 128)[:hidden]
+    near = h.abs() * (2.0 ** -16 + 2.0 ** -18)
+    far = near + torch.maximum((h.abs() + near) * 2.0 ** -4, grid)
+    pick, w_out = _picked(hidden, 100, g)
+    got = sjd.op_gated_mlp_f8(_rows(*ref.hold(x), width), _rows(*ref.hold(torch.cat((gate, up))), width), w_out, activation=act, dtype=dtype).cpu().double()
+    assert torch.equal(got, got[:1].expand_as(got))
+    want, far = h[pick], far[pick]
+    far = far if dtype is F32 else far + torch.finfo(dtype).eps / 2 * (want.abs() + far)
+    off = (got[0] - want).abs() / far
+    assert float(off.max()) <= 1, (float(off.max()), float(z[pick][off.argmax()]))
