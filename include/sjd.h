@@ -382,7 +382,9 @@ SJD_API int sjd_op_linear_f8(const sjd_f8 *rows, const sjd_f8 *weight, const flo
 
 /* The gated feed-forward block: w_in holds the F rows of the gate and then the F of `up`, hidden = activation(rows gate^T) * (rows up^T) is held in 8 bits, and
  * c_dev [rows->n_rows, w_out->n_rows] = hidden w_out^T as sjd_op_linear_f8 gives it; w_out->width = F <= 32768.  activation 0: x * sigmoid(x), 1: GELU (erf form), each within
- * 1e-5 of itself down to where sigmoid(x) or the normal distribution function is 2^-126, zero below.
+ * 1e-5 of itself down to where sigmoid(x) or the normal distribution function is 2^-126, zero below.  For float32 and half results the two sums are float32 sums of exact products; for bfloat16
+ * ones of many rows those of the 8-bit instruction, as above: a hidden value next to a border of the 8-bit grid may then land on the other side of it, which is 1.6e-3 of the results (2-norm) beside
+ * the 1.7e-3 of their rounding, at twice the speed where the chip is full.
  * The workspace, on a 16-byte boundary, is the call's own until its work has ended. */
 SJD_API int sjd_op_gated_mlp_f8(const sjd_f8 *rows, const sjd_f8 *w_in, const sjd_f8 *w_out, int activation, int dtype, void *c_dev, int64_t c_stride,
                                 int accumulate, void *workspace_dev, size_t workspace_bytes, void *hip_stream);

@@ -103,10 +103,11 @@ struct GatedF8 {
     float *loose;                   // [rows][loose_stride] where gated_f8_holds() is false: the hidden rows in float32, on their way
     int64_t loose_stride;           // the hidden channels rounded up to four
     int act;                        // 0 x * sigmoid(x), 1 GELU (erf)
-    bool exact;                     // products summed in float32 (see gemm_f8.hip)
+    int dtype;                      // of the results behind them, SJD_DTYPE_*: which sums the hidden rows are of (see gemm_f8.hip)
 };
 void launch_gated_f8(const GatedF8 &a, hipStream_t s);
-// Whether the product's own launch holds the hidden rows in 8 bits: it has whole groups of 128 channels to a tile, which takes rows enough to fill the chip.
-bool gated_f8_holds(const F8Rows &x, const F8Rows &w, bool exact);
+// Whether the product's own launch holds the hidden rows in 8 bits: it has whole groups of 128 channels in a workgroup, as the launch for few rows and short k and those for 16-bit
+// results that fill the chip do.
+bool gated_f8_holds(const F8Rows &x, const F8Rows &w, int dtype);
 
 }  // namespace sjd

@@ -143,6 +143,20 @@ template <int ROWS, int COLS> __device__ __forceinline__ void store_gated(float 
     }
 }
 
+// The same held in 8 bits; the tile has whole groups of 128 hidden channels, 16 neighbouring lanes to a group of a row.
+template <int ROWS, int COLS> __device__ __forceinline__ void hold_gated(const F8Rows &h, int act, const float *park, int m0, int n0, int tid, int threads) {
+    static_assert(COLS == 2 * kF8Group, "");
+    for (int p = tid; p < ROWS * (COLS / 16); p += threads) {
+        const int r = p / (COLS / 16), c = p % (COLS / 16) * 8;
+        if (m0 + r >= h.n_rows) continue;                          // whole groups leave
+        const float *at = park + r * pitch_of(COLS) + (c / 32) * 64 + c % 32;
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = n0 + c + e < h.width ? gate_of(at[e], act) * at[32 + e] : 0.f;
+        f8_hold8(h, m0 + r, n0 + c, y);
+    }
+}
+
 // What a kernel works on: C (a.c) or, of the gated block, the hidden rows: in 8 bits, or as float32 in `loose` on the way there.
 struct TileArgs {
     LinearF8 a;
@@ -160,7 +174,8 @@ struct TileArgs {
 // products in turn, and two such chains run beside each other.
 // What bounds it with one tile a CU is that chain, about 0.4 us a k-tile of 128 x 128 (the sizes at launch_tiles); 9945 x 1027 x 4096 in float32, 702 tiles on 512 places,
 // takes 99 us with the matrix unit busy 37% of it, 4096^3 with full rounds 1057 TFLOP/s of the bfloat16 instruction's 1270 in a library product.
-template <int BM, int BN, int ST, int KS, typename OutT, bool GATED, bool EXACT>
+// HELD: a tile of 256 has whole groups of 128 hidden channels and holds them in 8 bits itself.
+template <int BM, int BN, int ST, int KS, typename OutT, bool GATED, bool EXACT, bool HELD>
 __global__ __launch_bounds__(256 * KS) void f8_ring_kernel(TileArgs t) {
     constexpr int MI = BM / 64, NI = BN / 64;
     constexpr int LA = BM / 32, LB = BN / 32, LPW = LA + LB;   // 1 KB loads (8 rows x 128 bytes) per wave and k-tile
@@ -363,18 +378,19 @@ __global__ __launch_bounds__(256 * KS) void f8_ring_kernel(TileArgs t) {
         }
         __syncthreads();
     }
-    if constexpr (GATED) store_gated<BM, BN>(t.loose, t.loose_stride, x.n_rows, N, t.act, park, m0, n0, tid, 256 * KS);
+    if constexpr (HELD) hold_gated<BM, BN>(t.hidden, t.act, park, m0, n0, tid, 256 * KS);
+    else if constexpr (GATED) store_gated<BM, BN>(t.loose, t.loose_stride, x.n_rows, N, t.act, park, m0, n0, tid, 256 * KS);
     else store_tile<OutT, BM, BN, 256 * KS>(t.a, park, m0, n0, tid);
 }
 
-template <int BM, int BN, int ST, int KS, typename OutT, bool GATED, bool EXACT> void launch_ring(TileArgs t, hipStream_t s) {
+template <int BM, int BN, int ST, int KS, typename OutT, bool GATED, bool EXACT, bool HELD = false> void launch_ring(TileArgs t, hipStream_t s) {
     constexpr int cols = GATED ? BN / 2 : BN;
     const int outs = GATED ? t.a.w.n_rows / 2 : t.a.w.n_rows;
     t.tiles_n = (outs + cols - 1) / cols;
     t.n_tiles = (t.a.x.n_rows + BM - 1) / BM * t.tiles_n;
     constexpr int stages = KS * (ST * (BM + BN) * 128 + 2 * (BM + BN) * 4), park = BM * pitch_of(BN) * 4, smem = stages > park ? stages : park;
     static_assert(smem <= 160 * 1024, "");
-    auto kern = f8_ring_kernel<BM, BN, ST, KS, OutT, GATED, EXACT>;
+    auto kern = f8_ring_kernel<BM, BN, ST, KS, OutT, GATED, EXACT, HELD>;
     static std::atomic<uint64_t> allowed{0};
     allow_lds(reinterpret_cast<const void *>(kern), smem, allowed);
     kern<<<(t.n_tiles + 7) / 8 * 8, 256 * KS, smem, s>>>(t);
@@ -1015,8 +1031,8 @@ void launch_linear_f8(const LinearF8 &a, hipStream_t s) {
 
 // Which launch holds the hidden rows in 8 bits itself: it has whole groups of 128 channels.
 static bool gate_in_one(const F8Rows &x, const F8Rows &w) { return x.width <= 1024 && tiles(x.n_rows, w.n_rows, 32, 256) <= 256; }
-static bool gate_by_wide(const F8Rows &x, const F8Rows &w, bool exact) { return !exact && x.width > kF8Group && tiles(x.n_rows, w.n_rows, 256, 256) >= 256; }
-bool gated_f8_holds(const F8Rows &x, const F8Rows &w, bool exact) { return gate_in_one(x, w) || gate_by_wide(x, w, exact); }
+static bool gate_fills(const F8Rows &x, const F8Rows &w) { return x.width > kF8Group && tiles(x.n_rows, w.n_rows, 256, 256) >= 256; }
+bool gated_f8_holds(const F8Rows &x, const F8Rows &w, int dtype) { return gate_in_one(x, w) || (dtype != 0 && gate_fills(x, w)); }
 
 void launch_gated_f8(const GatedF8 &g, hipStream_t s) {
     LinearF8 a{};
@@ -1024,11 +1040,13 @@ void launch_gated_f8(const GatedF8 &g, hipStream_t s) {
     a.w = g.w;
     const TileArgs t{a, g.hidden, g.loose, g.loose_stride, g.act, 0, 0};
     if (gate_in_one(g.x, g.w)) return launch_gate(t, s);
-    if (gate_by_wide(g.x, g.w, g.exact)) return g.act ? launch_wide<float, true, 1>(t, s) : launch_wide<float, true, 0>(t, s);
     // A hidden value next to a border of the 8-bit grid goes to either side with what the 8-bit instruction drops, a step of 1/16 to 1/8 away: 1.6e-3 of the results over
-    // many values, but one of a few hundred may be half a percent.  Few tiles wait for memory and sum exact products in the same time (64 x 5632 x 1024 5.3 us and
-    // 5.4); tiles that multiply would take a quarter as long again (300 x 7682 x 1408 with the norms' launch 16.0 and 19.9).
-    if (g.exact || tiles(a.x.n_rows, a.w.n_rows, 32, 32) <= 512) launch_tiles<float, true, true>(t, s);
+    // many values, but one of a few hundred may be half a percent.  bfloat16 results are rounded by as much (1.7e-3), half ones by 2e-4: theirs, as float32 ones, sum exact products.
+    // Few tiles wait for memory and sum exact products in the same time (64 x 5632 x 1024 5.3 us and 5.4); tiles that multiply take a quarter as long
+    // again (300 x 7682 x 1408 with the norms' launch 16.0 and 19.9), and where the chip is full the block takes twice as long or more: 16384 x 1024, 2816 hidden 135 and 317, 4096 x 1024, 2816 52 and 97.
+    if (g.dtype == 1 && gate_fills(g.x, g.w)) return g.act ? launch_wide<float, true, 1>(t, s) : launch_wide<float, true, 0>(t, s);
+    if (g.dtype == 2 && gate_fills(g.x, g.w)) return launch_ring<128, 256, 3, 1, float, true, true, true>(t, s);
+    if (g.dtype != 1 || tiles(a.x.n_rows, a.w.n_rows, 32, 32) <= 512) launch_tiles<float, true, true>(t, s);
     else launch_tiles<float, true, false>(t, s);
     NormF8 n{};
     n.x = g.loose; n.x_stride = g.loose_stride; n.out = g.hidden;

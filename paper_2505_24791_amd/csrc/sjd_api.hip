@@ -1749,7 +1749,7 @@ size_t gated_workspace(GatedF8 *g, uint8_t *at) {
     size_t bytes = (size_t)(n * (codes + scales) + 15) / 16 * 16;
     g->loose = (float *)(at + bytes);
     g->loose_stride = (hidden + 3) / 4 * 4;
-    if (!gated_f8_holds(g->x, g->w, g->exact)) bytes += (size_t)n * g->loose_stride * 4;
+    if (!gated_f8_holds(g->x, g->w, g->dtype)) bytes += (size_t)n * g->loose_stride * 4;
     return bytes;
 }
 
@@ -1762,7 +1762,7 @@ int check_gated(const sjd_f8 *rows, const sjd_f8 *w_in, int dtype, GatedF8 *g) {
     if (w->n_rows < 2 || w->n_rows % 2) return fail(SJD_EINVAL, "w_in: needs as many rows of the gate as of up");
     if (w->n_rows / 2 > kNormF8Most) return fail(SJD_EINVAL, "w_in: at most %d hidden channels", kNormF8Most);
     if ((rc = check_tiles(x->n_rows, w->n_rows)) || (rc = check_whole_rows(x->n_rows, w->n_rows / 2))) return rc;
-    g->exact = dtype == SJD_DTYPE_F32;
+    g->dtype = dtype;
     gated_workspace(g, nullptr);
     if (g->hidden.scale_stride * g->hidden.n_rows > INT32_MAX) return fail(SJD_EINVAL, "too many rows for one call");
     return SJD_OK;

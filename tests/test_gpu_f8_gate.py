@@ -1,15 +1,18 @@
-"""The gated block of 8-bit rows where its hidden values are easily wrong: gates in the tail of the activation.
+"""The gated block of 8-bit rows where its hidden values are easily wrong: gates in the tail of the activation, results of three more bits than
+bfloat16's.
 
 Tolerances.  Hidden values lie on a grid of 8-bit floats: half a step, 2^-4 of a value or 2^-10 of a scale (at least the group's largest / 448).  The activation's float32 arithmetic
 is off by what the exponent of 2 is rounded by, 2^-24 of it twice and 2^-25 for its constant (it is at most 116 for the gates here: 2.5 * 116 * 2^-24 ln 2 < 2^-16), and by less than 2^-18 for the rest.
 Sums of integers are exact.
 """
+import math
+
 import pytest
 import torch
 
 import f8_reference as ref
 import paper_2505_24791_amd as sjd
-from test_gpu_f8 import BF16, F32, _gen, _rows
+from test_gpu_f8 import BF16, F16, F32, _gen, _rows
 
 pytestmark = pytest.mark.gpu
 
@@ -55,3 +58,22 @@ def test_a_group_of_gates_in_the_tail_keeps_its_bits(m, width, hidden, act, low,
     far = far if dtype is F32 else far + torch.finfo(dtype).eps / 2 * (want.abs() + far)
     off = (got[0] - want).abs() / far
     assert float(off.max()) <= 1, (float(off.max()), float(z[pick][off.argmax()]))
+
+
+@pytest.mark.parametrize("m,width,hidden", LAUNCHES + [(16400, 512, 1408), (9100, 520, 2307)])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_half_results_are_as_near_as_float32_sums_make_them(m, width, hidden, act):
+    """Against the hidden values of exact sums, held in float64's own way.  A value that is off by d of itself lands on the other side of a border of the grid with a probability of d over the
+    step, and is then off by a step.  Float32 sums of `width` products of either sign are off by about 2^-24 sqrt(width) <= 2^-19 of themselves, the activation by 2^-20: with a step of 2^-3.5, the
+    middle, about 2^-15 of the values cross, which is 2^-7.5 of a step, 2^-11, in 2-norm.  The result is rounded by up to 2^-11, evenly spread.  Both together, doubled: 2 * 2^-11 sqrt(1 + 1/3)."""
+    g = torch.Generator(device="cuda").manual_seed(m + hidden)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    rows, w_in = sjd.op_norm_f8(rand(m, width), norm="rms"), sjd.op_norm_f8(rand(2 * hidden, width) * width ** -0.5, norm="none")
+    w_out = sjd.op_norm_f8(rand(130, hidden) * hidden ** -0.5, norm="none")
+    got = sjd.op_gated_mlp_f8(rows, w_in, w_out, activation=act, dtype=F16)
+    at = torch.arange(0, m, max(1, m // 300))
+    val = lambda r, pick=None: ref.values(r.codes[slice(None) if pick is None else pick].cpu(), r.scales[slice(None) if pick is None else pick].cpu(), r.width)  # noqa: E731
+    z = val(rows, at.cuda()) @ val(w_in).T
+    h = ref.values(*ref.hold((ref.activation(z[:, :hidden], act) * z[:, hidden:]).float()), hidden)
+    want = h @ val(w_out).T
+    assert float((got[at.cuda()].cpu().double() - want).norm() / want.norm()) <= 2 * 2.0 ** -11 * math.sqrt(4 / 3)
