@@ -1,5 +1,5 @@
 """The gated block of 8-bit rows where its hidden values are easily wrong: gates in the tail of the activation, results of three more bits than
-bfloat16's.
+bfloat16's, results added to the stream; projections into the stream by every tile.
 
 Tolerances.  Hidden values lie on a grid of 8-bit floats: half a step, 2^-4 of a value or 2^-10 of a scale (at least the group's largest / 448).  The activation's float32 arithmetic
 is off by what the exponent of 2 is rounded by, 2^-24 of it twice and 2^-25 for its constant (it is at most 116 for the gates here: 2.5 * 116 * 2^-24 ln 2 < 2^-16), and by less than 2^-18 for the rest.
@@ -12,7 +12,7 @@ import torch
 
 import f8_reference as ref
 import paper_2505_24791_amd as sjd
-from test_gpu_f8 import BF16, F16, F32, _gen, _rows
+from test_gpu_f8 import BF16, F16, F32, TYPES, _gen, _integers_gpu, _rows
 
 pytestmark = pytest.mark.gpu
 
@@ -77,3 +77,49 @@ def test_half_results_are_as_near_as_float32_sums_make_them(m, width, hidden, ac
     h = ref.values(*ref.hold((ref.activation(z[:, :hidden], act) * z[:, hidden:]).float()), hidden)
     want = h @ val(w_out).T
     assert float((got[at.cuda()].cpu().double() - want).norm() / want.norm()) <= 2 * 2.0 ** -11 * math.sqrt(4 / 3)
+
+
+# 32x32 tiles (one and two a CU), 64x64 in two parts of k, 128x64, 64x64 and 128x64 several to a CU, 128x128 one and two to a CU
+@pytest.mark.parametrize("m,n", [(200, 300), (500, 900), (900, 1027), (1500, 1027), (700, 2901), (1300, 2051), (3000, 1203), (1300, 4099), (4001, 2003), (9001, 1027)])
+@pytest.mark.parametrize("k", [128, 700])
+def test_projection_into_the_stream_by_every_tile(m, n, k):
+    """Odd numbers of outputs, so that the last columns are a part of the last eight, in rows that begin anywhere in wider ones."""
+    xc, xs, x = _integers_gpu(m, m, k, top=2)
+    wc, ws, w = _integers_gpu(n, n, k, top=2)
+    bias = (torch.arange(n, device="cuda") % 13 - 6).float()
+    wide = (torch.arange(m * (n + 3), device="cuda") % 101 - 50).float().view(m, n + 3)
+    want = wide.double()
+    want[:, 1:1 + n] += x @ w.T + bias.double()
+    got = sjd.op_linear_f8(sjd.F8Rows(xc, xs, k), sjd.F8Rows(wc, ws, k), bias=bias, resid=wide[:, 1:1 + n])
+    assert got.data_ptr() == wide[:, 1:].data_ptr() and torch.equal(wide.double(), want)
+
+
+@pytest.mark.parametrize("m,width,hidden", LAUNCHES)
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_gated_block_into_the_stream_and_into_rows_of_a_larger_tensor(m, width, hidden, act):
+    """A gate that is 128 or nothing, `up` of small integers: hidden values are held as they are, and the weight behind them is of integers too."""
+    g = _gen(m + hidden)
+    n = 133
+    x = torch.zeros(m, width)
+    x[:, 0] = 1
+    x[:, 1:4] = torch.randint(-2, 3, (m, 3), generator=g)
+    gate = torch.zeros(hidden, width)
+    gate[:, 0] = torch.where(torch.rand(hidden, generator=g) < 0.3, -192.0, 128.0)
+    up = torch.zeros(hidden, width)
+    up[:, 1:4] = torch.randint(0, 2, (hidden, 3), generator=g)
+    w_out = torch.randint(-2, 3, (n, hidden), generator=g).float()
+    h = torch.clamp(x @ gate.T, min=0) * (x @ up.T)
+    assert torch.equal(ref.values(*ref.hold(h[:50]), hidden), h[:50].double())
+    want = (h.cuda().double() @ w_out.cuda().double().T)
+    rows, w_in, w_o = _rows(*ref.hold(x), width), _rows(*ref.hold(torch.cat((gate, up))), width), _rows(*ref.hold(w_out), hidden)
+    wide = (torch.arange(m * (n + 6), device="cuda") % 64 * 128.0).view(m, n + 6)
+    after = wide.double()
+    after[:, 2:2 + n] += want
+    got = sjd.op_gated_mlp_f8(rows, w_in, w_o, activation=act, resid=wide[:, 2:2 + n])
+    assert got.data_ptr() == wide[:, 2:].data_ptr() and torch.equal(wide.double(), after)
+    for dtype in TYPES:
+        out = torch.full((m + 2, n + 6), 3.0, dtype=dtype, device="cuda")
+        assert sjd.op_gated_mlp_f8(rows, w_in, w_o, activation=act, out=out[1:-1, 2:2 + n]).dtype is dtype
+        assert torch.equal(out[1:-1, 2:2 + n], want.to(F32).to(dtype))
+        out[1:-1, 2:2 + n] = 3
+        assert (out == 3).all()
