@@ -1020,8 +1020,7 @@ template <typename OutT, bool GATED, bool EXACT> void launch_tiles(const TileArg
 
 void launch_linear_f8(const LinearF8 &a, hipStream_t s) {
     const TileArgs t{a, {}, nullptr, 0, 0, 0, 0};
-    const int M = a.x.n_rows, N = a.w.n_rows;
-    if (wide_takes(a) && (tiles(M, N, 256, 256) >= 256 || (tiles(M, N, 128, 128) > 512 && gemm_p8_one_round(M, N)))) {
+    if (wide_takes(a) && f8_wide_before_tiles(a.x.n_rows, a.w.n_rows)) {
         if (a.dtype == 1) launch_wide_rows<bf16>(t, s);
         else launch_wide_rows<f16>(t, s);
     } else if (a.dtype == 0) launch_tiles<float, false, true>(t, s);
@@ -1031,7 +1030,7 @@ void launch_linear_f8(const LinearF8 &a, hipStream_t s) {
 
 // Which launch holds the hidden rows in 8 bits itself: it has whole groups of 128 channels.
 static bool gate_in_one(const F8Rows &x, const F8Rows &w) { return x.width <= 1024 && tiles(x.n_rows, w.n_rows, 32, 256) <= 256; }
-static bool gate_fills(const F8Rows &x, const F8Rows &w) { return x.width > kF8Group && tiles(x.n_rows, w.n_rows, 256, 256) >= 256; }
+static bool gate_fills(const F8Rows &x, const F8Rows &w) { return x.width > kF8Group && f8_gate_fills(x.n_rows, w.n_rows / 2); }
 bool gated_f8_holds(const F8Rows &x, const F8Rows &w, int dtype) { return gate_in_one(x, w) || (dtype != 0 && gate_fills(x, w)); }
 
 void launch_gated_f8(const GatedF8 &g, hipStream_t s) {

@@ -50,4 +50,24 @@ inline bool gemm_dma_before_ring(int M, int N, bool gelu) {
     return (gelu ? 1.78 : 1.68) * rounds(large / 256.0, 0.5, 0.45) < rounds(small / 512.0, 0.25, 0.75);
 }
 
+// 8-bit projections with 16-bit results, on the kernel that walks over 256x256 tiles (gemm_f8.hip), which deals whole row panels to the XCDs, or on two 128x128 tiles (or several smaller ones) to a
+// CU, which spread over the chip: a round of the former takes as long as 2.3 to 2.7 of its tiles a CU would in the latter (k = 1024; 2.1 with k = 4096), so it is taken while the rounds of
+// its fullest XCD are at most two and a half times what spreads.  us, tiles that walk / that spread, k = 1024 (4096): one panel, 1 x 128256 194.7 / 34.1, 64 x 128256 200.5 / 38.3, 256 x 128256 226.3 /
+// 71.7, 256 x 65536 103.6 / 34.7; two, 512 x 65536 109.4 / 64.0; three, 768 x 32768 56.2 / 50.4 (201.3 / 143.4); four, 1024 x 16384 32.1 / 34.5 (88.0 / 89.7), 1024 x 16640 41.9 / 40.7 (123.7 /
+// 115.3); nine, 2304 x 8448 42.0 / 41.4 (126.5 / 115.7), 2304 x 8192 32.7 / 40.2; 33000 x 260 34.6 / 25.6, 16640 x 1028 35.6 / 35.9, 4352 x 5632 41.7 / 46.2, 8448 x 4096 45.2 / 64.1.
+inline bool f8_wide_before_tiles(int M, int N) {
+    const long long large = (((long long)M + 255) / 256) * (((long long)N + 255) / 256), small = (((long long)M + 127) / 128) * (((long long)N + 127) / 128);
+    const long long rounds = (tiles_of_fullest_xcd(M, N, kP8Tile, kP8Tile) + kCusPerXcd - 1) / kCusPerXcd;
+    return (large >= kXcds * kCusPerXcd && rounds * 2048 <= small * 5) || (small > 512 && rounds == 1);
+}
+
+// The first half of the gated block with F hidden channels, the same way: the tiles that spread leave float32 behind for another launch, so the bound is three.  us, k = 1024 (4096): 512 x 16384 hidden
+// 73.9 / 59.0 (221.8 / 133.0), 768 x 16384 75.2 / 77.4 (224.4 / 173.2), 1024 x 8320 53.9 / 60.4 (133.5 / 135.5), 2304 x 4224 51.1 / 58.6 (135.2 / 133.2), 4352 x 2816 52.0 / 65.5 (137.4 / 137.9).
+inline bool f8_gate_fills(int M, int F) {
+    const int N = 2 * F;
+    const long long large = (((long long)M + 255) / 256) * (((long long)N + 255) / 256), small = (((long long)M + 127) / 128) * (((long long)N + 127) / 128);
+    const long long rounds = (tiles_of_fullest_xcd(M, N, kP8Tile, kP8Tile) + kCusPerXcd - 1) / kCusPerXcd;
+    return large >= kXcds * kCusPerXcd && rounds * 1024 <= small * 3;
+}
+
 }  // namespace sjd
