@@ -70,4 +70,11 @@ inline bool f8_gate_fills(int M, int F) {
     return large >= kXcds * kCusPerXcd && rounds * 1024 <= small * 3;
 }
 
+// Reading 8-bit rows back: lanes a row, one for every eight values up to a workgroup of 256, fewer where a launch would have more than 2^31 threads (they go over the row in turns).
+inline int f8_read_lanes(int width, int n_rows) {
+    int lanes = 8;
+    while (lanes < 256 && lanes * 8 < width && (long long)n_rows * lanes * 2 < (1ll << 31)) lanes *= 2;
+    return lanes;
+}
+
 }  // namespace sjd

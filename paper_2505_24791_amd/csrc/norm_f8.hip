@@ -7,6 +7,7 @@
 // Everything between h and the rounding to float32 is float64: a value next to a border of the 8-bit grid then goes to its side in whatever order sums
 // are taken.  The vector unit does float64 at the rate of float32, and the kernel moves bytes: each row is read once, held in registers, written once.
 #include "f8.h"
+#include "gemm_rules.h"
 
 namespace sjd {
 
@@ -216,9 +217,7 @@ template void launch_norm_f8<bf16>(const NormF8 &, bool, hipStream_t);
 template void launch_norm_f8<f16>(const NormF8 &, bool, hipStream_t);
 
 template <typename T> void launch_f8_read(const F8Rows &r, T *out, int64_t stride, hipStream_t s) {
-    int lanes = 8;
-    while (lanes < 256 && lanes * 8 < r.width) lanes *= 2;
-    const int per = 256 / lanes;
+    const int lanes = f8_read_lanes(r.width, r.n_rows), per = 256 / lanes;
     f8_read_kernel<T><<<(int)(((int64_t)r.n_rows + per - 1) / per), 256, 0, s>>>(r, out, stride, lanes);
 }
 template void launch_f8_read<float>(const F8Rows &, float *, int64_t, hipStream_t);

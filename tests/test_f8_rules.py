@@ -12,6 +12,7 @@ SOURCE = r"""
 extern "C" {
 int wide(int M, int N) { return sjd::f8_wide_before_tiles(M, N); }
 int gate_wide(int M, int F) { return sjd::f8_gate_fills(M, F); }
+int read_lanes(int width, int n_rows) { return sjd::f8_read_lanes(width, n_rows); }
 }
 """
 
@@ -54,3 +55,21 @@ def test_the_fullest_xcd_decides(rules):
             one_round = rounds == 1 and small > 512
             assert rules.wide(M, N) == (one_round or (large >= 256 and rounds <= 2.5 * small / 1024)), (M, N)
             assert rules.gate_wide(M, N // 2) == (large >= 256 and rounds <= 3 * small / 1024), (M, N)
+
+
+def _whole_rows(width):
+    """Threads a row that the library counts before it accepts a call over whole rows."""
+    return 16 if width <= 128 else 32 if width <= 256 else 64 if width <= 1024 else 256 if width <= 2048 else 512 if width <= 8192 else 1024
+
+
+def test_reading_back_launches_no_more_threads_than_are_counted(rules):
+    """Threads of a launch are counted in 32 bits: up to as many rows as the library accepts, a launch of whole workgroups of 256 has at most 2^31."""
+    for width in (1, 8, 64, 65, 128, 129, 256, 257, 512, 513, 640, 1000, 1024, 1025, 2048, 2049, 8192, 32768, 1 << 20):
+        most = (2 ** 31 - 1) // _whole_rows(width)
+        for n in (1, 5, 4096, 100000, most // 3, most - 1, most):
+            lanes = rules.read_lanes(width, n)
+            assert 8 <= lanes <= 256 and lanes & (lanes - 1) == 0
+            assert -(-n // (256 // lanes)) * 256 <= 2 ** 31, (width, n, lanes)
+    # rows that are not so many: a lane for every eight values, up to a workgroup
+    for width, lanes in ((1, 8), (64, 8), (65, 16), (512, 64), (513, 128), (1024, 128), (1025, 256), (32768, 256)):
+        assert rules.read_lanes(width, 100000) == lanes

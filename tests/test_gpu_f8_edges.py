@@ -281,3 +281,22 @@ def test_a_weight_whose_storage_is_replaced():
     assert torch.equal(sjd.op_linear_f8(rows, weight, dtype=F32).double(), x[2] @ a[2].T)
     weight.codes.data, weight.scales.data = b[0], b[1]
     assert torch.equal(sjd.op_linear_f8(rows, weight, dtype=F32).double(), x[2] @ b[2].T)
+
+
+def test_as_many_rows_as_are_read_back_at_once():
+    """2^25 - 1 rows of 640, the most of that width: the first, the last and some between differ from the others."""
+    n, width = (1 << 25) - 1, 640
+    _room(72)
+    codes = torch.full((n, width), 0x38, dtype=torch.uint8, device="cuda")
+    scales = torch.full((n, 8), 127, dtype=torch.uint8, device="cuda")
+    marks = [0, 1, n // 2, n // 2 + 1, n - 3, n - 2, n - 1]
+    for i, r in enumerate(marks):
+        codes[r, i::3] = 0x40 + 8 * i                                      # 2, 4, 8 ..
+        scales[r, i % 5] = 120
+    out = torch.empty((n, width), dtype=F16, device="cuda")
+    sjd.op_f8_read(sjd.F8Rows(codes, scales, width), F16, out=out)
+    want = ref.values(codes[marks].cpu(), scales[marks].cpu(), width).half()
+    assert torch.equal(out[marks].cpu(), want)
+    out[marks] = 1
+    for a in range(0, n, 1 << 22):
+        assert bool((out[a:a + (1 << 22)] == 1).all()), a
