@@ -352,7 +352,8 @@ SJD_API int sjd_op_kv4_attention(const sjd_kv4 *cache, const sjd_kv4_attention *
  * n_rows rows of `width` values (a weight's rows are its outputs, its width its inputs).  codes: e4m3 (4 exponent bits, bias 7, 3 mantissa
  * bits, largest 448, no infinities), each row padded with ZEROS to a multiple of 128; 128 consecutive values share a power of two s = 2^e, scales: the byte e + 127, one for each
  * 128 values.  What sjd_op_norm_f8 writes has the smallest s with max |x| <= 448 s over a group's finite values, -120 <= e <= 120, and x / s to nearest even;
- * values that are not finite become NaN.  Rows from elsewhere may have any e in that range.  codes on a 16-byte
+ * values that are not finite become NaN.  Rows from elsewhere may have any e in that range; codes from 256 on with e = 120 are 2^128 and more, which float32 does not have: read back, and in
+ * sums of exact products (below), they are infinite.  codes on a 16-byte
  * boundary, scales on a 4-byte one; code_stride, in bytes, is a multiple of 16, at least the padded width, up to 2^22; scale_stride is a multiple of 4, at least the
  * number of groups, up to 2^20.  width <= 2^20, n_rows <= 2^30, n_rows * scale_stride < 2^31; a projection has fewer than 2^23 tiles of 128 rows by
  * 128 outputs, a call over whole rows (norms, reading, the gated block's hidden rows) fewer than 2^21 rows, 2^27 where they are at most 128 wide. */

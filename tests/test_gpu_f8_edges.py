@@ -300,3 +300,26 @@ def test_as_many_rows_as_are_read_back_at_once():
     out[marks] = 1
     for a in range(0, n, 1 << 22):
         assert bool((out[a:a + (1 << 22)] == 1).all()), a
+
+
+@pytest.mark.parametrize("m,n,k", [(4, 40, 128), (40, 300, 256), (900, 1027, 256), (3000, 1203, 256), (9000, 2304, 256)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scales_at_the_ends_of_their_range(m, n, k, dtype):
+    """One product a result, of scales 2^e and 2^-e: exact down to the smallest code with e = -120, and up to what float32 has; beyond that infinite where products are exact (float32)."""
+    codes = torch.tensor([0x01, 0x02, 0x03, 0x05, 0x07, 0x08, 0x0f, 0x38, 0x70, 0x77, 0x78, 0x7d, 0x7e, 0x81, 0xfe], dtype=torch.uint8)
+    for e in (-120, -119, -118, 118, 119, 120):
+        xc, wc = torch.zeros((m, k), dtype=torch.uint8), torch.zeros((n, k), dtype=torch.uint8)
+        xc[:, 3], wc[:, 3] = codes[torch.arange(m) % len(codes)], codes[torch.arange(n) // 3 % len(codes)]
+        xs, ws = torch.full((m, 4), 127 + e, dtype=torch.uint8), torch.full((n, 4), 127 - e, dtype=torch.uint8)
+        x, w = ref.values(xc, xs, k), ref.values(wc, ws, k)
+        want = x[:, 3:4] * w[:, 3]
+        if dtype is F32:
+            x, w = (torch.where(v.abs() >= 2.0 ** 128, math.inf * v.sign(), v) for v in (x[:, 3:4], w[:, 3]))
+            far = torch.isinf(x) | torch.isinf(w)
+            want = torch.where(far, math.nan, want)                        # beside zeros in the other channels: infinite or not a number
+        want = want.to(F32).to(dtype)
+        got = sjd.op_linear_f8(_rows(xc, xs, k), _rows(wc, ws, k), dtype=dtype).cpu()
+        fine = ~torch.isnan(want)
+        assert torch.equal(got[fine], want[fine]), e
+        assert not torch.isfinite(got[~fine]).any(), e
+        assert m < len(codes) or bool((~fine).any()) == (dtype is F32 and abs(e) == 120), e        # all codes are there
