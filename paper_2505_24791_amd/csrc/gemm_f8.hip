@@ -404,7 +404,7 @@ template <int BM, int BN, int ST, int KS, typename OutT, bool GATED, bool EXACT,
 // runs on into the next tile.  The scales of four k-tiles, a dword a row, take turns in two places behind the ring.
 // The weight is the left operand of the instruction, so that a lane's registers are one row's outputs, four consecutive ones at a time: halves of a wave swap
 // registers and hold sixteen bytes each, and results go to memory without LDS; of the gated block a row's largest is mostly found in a lane.
-// us in a row of calls: 8192^3 406, 2710 TFLOP/s, bound by power (1.8 GHz, the matrix unit busy 72% of the cycles); 32768 x 4096 x 1024 130, bound by its 268 MB of results, which leave
+// us in a row of calls: 8192^3 406 to 439 by card, 2500 to 2710 TFLOP/s, bound by power (1.8 GHz, the matrix unit busy 72% of the cycles); 32768 x 4096 x 1024 130, bound by its 268 MB of results, which leave
 // all CUs at once (112 without the stores); 16384 x 1024 with 2816 hidden channels 97 and 44 under the profiler, the gate's activations on the vector unit.  Two workgroups of 128 x 128 tiles of
 // the kernel above read each operand twice as often.
 constexpr int W_UNITS = 9, W_UNIT = 16 * 1024, W_SCALES = W_UNITS * W_UNIT, W_MORE = W_SCALES + 2 * 512 * 4;
@@ -851,9 +851,11 @@ template <int ST, typename OutT, bool GATED, bool EXACT> void launch_thin(const 
 // ------------------------------------------------------------------------------------------------
 // The gate for few rows and short k in one launch: 32 rows by 128 hidden channels, which is one scale, a workgroup; each of its eight waves has the 32 weight rows
 // of 16 channels (gate, then up) in a ring of its own, the rows of x are shared.  A launch less than tiles that leave float32 behind for norm_f8.hip to hold; for k
-// beyond 1024 its 288 bytes of a k from memory take one CU longer than those two launches.  What bounds it is those bytes, at 50 KB a microsecond.  The whole block, us in a row of calls (in a
-// graph), with the two launches -> this: 64 x 1024, 2816 hidden 13.5 (13.4) -> 14.0 (14.2), where operands are wrapped anew for every call 17.9 -> 14.7; 300 x 1024, 2816 22.0 (22.4) -> 17.4 (17.6);
-// 64 x 512, 1300 13.7 (10.0) -> 11.1 (10.3); one row of 1024, 2816 13.7 (11.3) -> 13.1 (13.2).
+// beyond 1024 its 288 bytes of a k from memory take one CU longer than those two launches.  What bounds it is those bytes, at 50 KB a microsecond.  The whole block, us in a graph / in calls with
+// kept operands / with operands wrapped anew, two launches -> this: 64 x 256, 2816 hidden 11.1 / 14.1 / 17.1 -> 10.2 / 11.3 / 14.2; 64 x 512, 1300 10.2 / 13.9 / 17.2 -> 10.4 / 11.4 / 14.3; 1 x 512, 2816
+// 10.1 / 13.7 / 17.3 -> 10.6 / 11.3 / 14.0; one row of 1024, 2816 11.3 / 13.7 / 17.2 -> 13.2 / 13.1 / 14.4; 64 x 1024, 2816 13.2 / 14.3 / 17.0 -> 14.1 / 13.9 / 14.2; 200 x 1024, 2816 18.0 / 18.0 / 18.3 ->
+// 15.0 / 14.6 / 14.8; 300 x 1024, 2816 20.0 / 19.6 / 19.9 -> 17.4 / 17.1 / 17.1.  Calls outside of a graph, which wait for the host, are as short or shorter everywhere; in a graph it wins with k up to 256, from 64 workgroups
+// with 512 and from 88 with 1024, and with fewer it loses, 1.33 times at the most (1 x 1024, 256 hidden 8.2 -> 10.9).  One rule for both: a captured call has the bits and the workspace of an eager one.
 template <int ST> __global__ __launch_bounds__(512) void f8_gate_kernel(TileArgs t) {
     constexpr int STB = (32 + 256) * 128, SCALES = ST * STB, LARGEST = SCALES + 2 * 8 * 256;
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -991,7 +993,7 @@ bool wide_takes(const LinearF8 &a) { return a.dtype != 0 && a.x.width > kF8Group
 
 int64_t tiles(int64_t rows, int64_t outs, int bm, int bn) { return (rows + bm - 1) / bm * ((outs + bn - 1) / bn); }
 
-// Whatever is not for the persistent kernel: the smallest tile of which no CU has more than one (two of the smallest), or two or three with a shorter ring where that
+// Whatever is not for the persistent kernel, by the 256 CUs of this chip: the smallest tile of which no CU has more than one (two of the smallest), or two or three with a shorter ring where that
 // fills more of the chip than the next larger tile; at last two workgroups with 128x128 tiles to a CU.  A tile of half the size reads more of both operands, but time is what one CU gets through while it walks k.  us, M x N x K, the weight from memory, as thin / 64x64 /
 // 128x64 / 128x128 with one workgroup to a CU / with two: 64 x 1024 x 2816 5.1 / 8.5 / 11.2 / 15.6 / 22.3; 16 x 8192 x 8192 17.4 / 22.8 / 26.3 / 41.8 / 76.0;
 // 512 x 1024 x 4096 9.9 / 11.1 / 15.1 / 21.0 / 31.4; 256 x 2304 x 768 6.1 / 5.6 / 6.3 / 8.2 / 9.7; 1024 x 1024 x 4096 - / 11.6 / 15.2 / 21.1 / 31.5; 512 x 4096 x 1024 - / 11.4 / 7.7 / 9.6 / 12.0;
