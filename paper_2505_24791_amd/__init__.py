@@ -507,7 +507,8 @@ _parting = threading.Lock()
 class F8Rows:
     """Rows, or a weight [outputs, inputs], in 8 bits (``sjd_f8``): ``codes`` [rows, width rounded up to 128] (uint8 or float8_e4m3fn), zeros after
     ``width``, and ``scales`` uint8 [rows, groups of 128 rounded up to 4], a power of two 2^(byte - 127) for each 128 values.  Made by ``op_norm_f8`` (of a
-    weight: ``norm="none"``) or held by the caller.  A call takes the tensors as they are then; rows of a larger tensor (``codes[a:b]``) are fine."""
+    weight: ``norm="none"``) or held by the caller.  A call takes the tensors as they are then; rows of a larger tensor (``codes[a:b]``) are fine.  Threads may
+    share an object; one that replaces both tensors while others call replaces the object instead, for ``codes`` and ``scales`` are set one after the other."""
 
     __slots__ = ("_codes", "_scales", "_width", "_both", "_made")
 

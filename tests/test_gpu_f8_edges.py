@@ -323,3 +323,26 @@ def test_scales_at_the_ends_of_their_range(m, n, k, dtype):
         assert torch.equal(got[fine], want[fine]), e
         assert not torch.isfinite(got[~fine]).any(), e
         assert m < len(codes) or bool((~fine).any()) == (dtype is F32 and abs(e) == 120), e        # all codes are there
+
+
+@pytest.mark.parametrize("m,n", [(1, 128257), (64, 65536), (300, 40000), (700, 33000)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_few_rows_by_many_outputs(m, n, dtype):
+    """One to three panels of 256 rows, which the kernel that walks over tiles would leave to as many XCDs; the gate too."""
+    k = 256
+    xc, xs, x = _integers_gpu(m, m, k)
+    wc, ws, w = _integers_gpu(n, n, k)
+    bias = (torch.arange(n, device="cuda") % 13 - 6).float()
+    got = sjd.op_linear_f8(sjd.F8Rows(xc, xs, k), sjd.F8Rows(wc, ws, k), bias=bias, dtype=dtype)
+    assert torch.equal(got, (x @ w.T + bias.double()).to(F32).to(dtype))
+    hidden = min(n // 2, 16400)
+    g = _gen(n)
+    (gc, gs), (ic, is_) = _gate_integers(g, min(m, 60), k, hidden)
+    at = torch.arange(m) % min(m, 60)
+    z = ref.values(gc, gs, k) @ ref.values(ic, is_, k).T
+    held = ref.values(*ref.hold(torch.clamp(z[:, :hidden], min=0) * z[:, hidden:]), hidden)
+    pick = torch.randint(0, hidden, (90,), generator=g)
+    w_out = torch.zeros(90, hidden)
+    w_out[torch.arange(90), pick] = 1
+    got = sjd.op_gated_mlp_f8(_rows(gc[at], gs[at], k), _rows(ic, is_, k), _rows(*ref.hold(w_out), hidden), dtype=dtype).cpu()
+    assert torch.equal(got, held[:, pick].to(F32).to(dtype)[at])
